@@ -40,7 +40,8 @@ typedef enum {
     BM_ERR_DTYPE = -3,      /* dtype is neither BM_F32 nor BM_BF16                  */
     BM_ERR_WORKSPACE = -4,  /* workspace NULL, misaligned or smaller than required  */
     BM_ERR_BAD_TABLE = -5,  /* bm_validate_tables: entry outside [-1,E) or == row   */
-    BM_ERR_HIP = -6         /* a kernel launch failed (hipGetLastError != success)  */
+    BM_ERR_HIP = -6,        /* a kernel launch failed (hipGetLastError != success)  */
+    BM_ERR_ALIGN = -7       /* 8-bit operators: an array is off its required boundary */
 } bm_status;
 
 typedef enum { BM_F32 = 0, BM_BF16 = 1 } bm_dtype;
@@ -298,6 +299,114 @@ int bm_pack_weights(const bm_layer_desc *desc, const bm_weights *weights,
  * With d = 0 and F = 0 it is the scratch of bm_permute_by_expert alone, a function
  * of T, E and K. */
 size_t bm_workspace_bytes(const bm_layer_desc *desc);
+
+/* ---- 8-bit operators -----------------------------------------------------------
+ *
+ * Values in 8 bits are e4m3 (1 sign, 4 exponent, 3 mantissa bits, largest 448, no
+ * infinities), one byte each.  They stand for q * scale with one fp32 scale for each
+ * block of 128 consecutive values of a row (activations: [rows][ceil(cols/128)]) or
+ * for each 128 x 128 block of a matrix (weights: [n][ceil(rows/128)][ceil(cols/128)]);
+ * the last blocks may be cut.  A block with largest magnitude m has
+ *   scale = max(m / 448, 2^-126),  q = e4m3(x / scale)
+ * both quotients rounded to fp32, q rounded to nearest even.  A block that holds an
+ * infinity or a NaN gets a NaN scale and NaN values.
+ *
+ * The entry points follow the conventions above (caller's stream, no allocation, host
+ * checks first) and can be captured into a HIP graph.  8-bit arrays that a product
+ * reads or writes must be 16-byte aligned (BM_ERR_ALIGN otherwise). */
+
+typedef struct {
+    int32_t n, rows, cols;   /* n matrices [rows][cols]; a count of 0 makes the call a no-op */
+    int32_t block_rows;      /* 1: a scale per row and 128 values; 128: per 128 x 128 block  */
+    int32_t dtype;           /* of src: BM_F32 or BM_BF16                                    */
+} bm_quantize_desc;
+
+/* q [n][rows][cols] and scale [n][rows / block_rows, rounded up][ceil(cols/128)] of
+ * src [n][rows][cols] (all device).  Weights are quantized once, at load time; any
+ * width is taken, whole 16-byte pieces at a time where cols is a multiple of 8 and the
+ * arrays are aligned. */
+int bm_quantize(const bm_quantize_desc *desc, const void *src, void *q, float *scale, void *stream);
+
+typedef struct {
+    int32_t T, d;            /* rows and width, 1 <= d <= 16384                              */
+    int32_t dtype;           /* of x, residual, gamma, residual_out, y: BM_F32 or BM_BF16    */
+    float eps;               /* >= 0, added to the mean square                               */
+} bm_norm_desc;
+
+/* What stands in front of the layer:
+ *   r = x + residual,  n = r / sqrt(mean_j r_j^2 + eps) * gamma      (fp32, per row)
+ * residual_out [T][d] = r and y [T][d] = n rounded to dtype; q [T][d] and scale
+ * [T][ceil(d/128)] = the 8-bit form of the fp32 n.  residual NULL stands for zeros; any
+ * of residual_out, y and the pair q, scale may be NULL, not all three.  residual_out may
+ * be residual or x, y may be x or residual (not the same array as residual_out).
+ * All device. */
+int bm_add_rmsnorm(const bm_norm_desc *desc, const void *x, const void *residual, const void *gamma,
+                   void *residual_out, void *y, void *q, float *scale, void *stream);
+
+typedef struct {
+    int32_t rows;            /* rows of the output, at least offsets[E]                      */
+    int32_t a_rows;          /* rows of a                                                    */
+    int32_t N, Kd;           /* output width and reduction, multiples of 32, Kd <= 32768     */
+    int32_t E;               /* groups, 1 <= E <= BM_MAX_E                                   */
+    int32_t K;               /* output row i reads row row_map[i] / K of a                   */
+    int32_t dtype;           /* of c: BM_F32 or BM_BF16 (not read by bm_grouped_swiglu)      */
+} bm_product_desc;
+
+/* Rows grouped by expert, each group with its own matrix:
+ *   c[i][n] = sum_k a[r(i)][k] * w[e][n][k]   for offsets[e] <= i < offsets[e+1]
+ * a [a_rows][Kd] 8-bit with a_scale [a_rows][ceil(Kd/128)], w [E][N][Kd] 8-bit with
+ * w_scale [E][ceil(N/128)][ceil(Kd/128)], c [rows][N] (all device).  r(i) = row_map[i] / K
+ * (row_map [rows] device int32: bm_permute_by_expert's perm with the layer's K), or i
+ * with row_map NULL (a_rows >= rows then).  offsets [E+1] device int32, or NULL with
+ * E = 1: one group of all rows.  Products of a block of 128 are summed by the matrix
+ * unit in fp32, blocks are scaled and added in fp32 in order; c is rounded once.  Rows of
+ * c behind offsets[E] are left as they were, groups without rows read nothing.  Offsets
+ * are taken as clamped to [0, rows], mapped rows as clamped to [0, a_rows).
+ * Equal calls give equal bits. */
+int bm_grouped_matmul(const bm_product_desc *desc, const void *a, const float *a_scale, const int32_t *row_map,
+                      const int32_t *offsets, const void *w, const float *w_scale, void *c, void *stream);
+
+/* Two such products and what an expert does with them:
+ *   h[i] = silu(a[r(i)] . w_gate[e]) * (a[r(i)] . w_up[e])          (fp32)
+ * written as 8-bit h [rows][N] with h_scale [rows][ceil(N/128)]: the input of
+ * bm_grouped_matmul with the down matrices. */
+int bm_grouped_swiglu(const bm_product_desc *desc, const void *a, const float *a_scale, const int32_t *row_map,
+                      const int32_t *offsets, const void *w_gate, const float *gate_scale, const void *w_up,
+                      const float *up_scale, void *h, float *h_scale, void *stream);
+
+/* Weights of a layer whose experts are held in 8 bits (half the memory of bf16: twice as
+ * many resident experts), all device pointers; shapes as in bm_weights, scales per
+ * 128 x 128 block.  Router weights and bias stay in bf16 and fp32.  Rows and scales of an
+ * expert that is not resident are never read. */
+typedef struct {
+    const void *w_router;                          /* [E][d] bf16                        */
+    const float *router_bias;                      /* [E], or NULL                       */
+    const void *w_gate;  const float *gate_scale;  /* [E][F][d]                          */
+    const void *w_up;    const float *up_scale;    /* [E][F][d]                          */
+    const void *w_down;  const float *down_scale;  /* [E][d][F]                          */
+    const void *ws_gate; const float *ws_gate_scale;   /* [n_shared][F][d], NULL if none */
+    const void *ws_up;   const float *ws_up_scale;
+    const void *ws_down; const float *ws_down_scale;   /* [n_shared][d][F]               */
+    const float *buddy_q;                          /* as in bm_weights                   */
+} bm_quantized_weights;
+
+/* bm_moe_forward on such weights: the same routing, substitution, grouping and
+ * aggregation (same ids, offsets and gate weights, same flags), the experts by way of
+ * bm_grouped_swiglu and bm_grouped_matmul.  desc->dtype is BM_BF16 (of x, w_router and,
+ * without BM_Y_F32, y).  x_q [T][d], x_scale [T][ceil(d/128)]: the 8-bit form of the
+ * tokens that the experts read, as bm_add_rmsnorm writes it; both NULL: the call makes it
+ * from x.  Every expert's output is held in fp32 up to 256 tokens and in bf16 beyond.
+ * workspace: device scratch, 256-byte aligned, of at least
+ * bm_workspace_bytes_quantized(desc) bytes (one sized for a larger T of the layer is
+ * enough).  d and F at most 32768.  Equal calls give equal bits; a token's y can differ
+ * in its last bits with the rest of the batch. */
+int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale,
+                             const bm_quantized_weights *weights, const uint64_t *residency_bitmap,
+                             const int32_t *buddy_table, void *y, void *workspace, size_t workspace_bytes,
+                             const bm_debug_out *dbg, void *stream);
+
+/* Its scratch (host, pure function of desc; 0 if desc is invalid). */
+size_t bm_workspace_bytes_quantized(const bm_layer_desc *desc);
 
 /* Host-side check of a residency bitmap and buddy table (host pointers):
  * every table entry is -1 or in [0,E) and differs from its row index

@@ -12,4 +12,6 @@ from .binding import (  # noqa: F401
     BM_STATIC_WORKSPACE_BYTES,
     bm_workspace_bytes, bm_validate_tables, bm_strerror, library_path, load_library,
     bm_packed_bytes, bm_pack_weights, bm_coactivation_accumulate, bm_build_buddy_table, bm_stream_read,
+    QuantizeDesc, NormDesc, ProductDesc, QuantizedWeights, make_quantized_weights,
+    bm_quantize, bm_add_rmsnorm, bm_grouped_matmul, bm_grouped_swiglu, bm_moe_forward_quantized, bm_workspace_bytes_quantized,
 )

@@ -41,6 +41,24 @@ class DebugOut(ctypes.Structure):
                [("stage_events", ctypes.c_void_p * 5)]
 
 
+class QuantizeDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n", "rows", "cols", "block_rows", "dtype")]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class ProductDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "a_rows", "N", "Kd", "E", "K", "dtype")]
+
+
+class QuantizedWeights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in
+                ("w_router", "router_bias", "w_gate", "gate_scale", "w_up", "up_scale", "w_down", "down_scale",
+                 "ws_gate", "ws_gate_scale", "ws_up", "ws_up_scale", "ws_down", "ws_down_scale", "buddy_q")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -76,6 +94,16 @@ def load_library() -> ctypes.CDLL:
         lib.bm_moe_forward_static.restype = i32
         lib.bm_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
         lib.bm_stream_read.restype = i32
+        lib.bm_quantize.argtypes = [ctypes.POINTER(QuantizeDesc), vp, vp, vp, vp]
+        lib.bm_add_rmsnorm.argtypes = [ctypes.POINTER(NormDesc)] + [vp] * 8
+        lib.bm_grouped_matmul.argtypes = [ctypes.POINTER(ProductDesc)] + [vp] * 8
+        lib.bm_grouped_swiglu.argtypes = [ctypes.POINTER(ProductDesc)] + [vp] * 11
+        lib.bm_moe_forward_quantized.argtypes = [ctypes.POINTER(LayerDesc), vp, vp, vp, ctypes.POINTER(QuantizedWeights), vp, vp,
+                                                 vp, vp, ctypes.c_size_t, ctypes.POINTER(DebugOut), vp]
+        lib.bm_workspace_bytes_quantized.restype = ctypes.c_size_t
+        lib.bm_workspace_bytes_quantized.argtypes = [ctypes.POINTER(LayerDesc)]
+        for f in (lib.bm_quantize, lib.bm_add_rmsnorm, lib.bm_grouped_matmul, lib.bm_grouped_swiglu, lib.bm_moe_forward_quantized):
+            f.restype = i32
         for f in (lib.bm_validate_tables, lib.bm_route_topk, lib.bm_buddy_remap, lib.bm_permute_by_expert,
                   lib.bm_moe_forward, lib.bm_coactivation_accumulate, lib.bm_build_buddy_table):
             f.restype = i32
@@ -204,3 +232,51 @@ def bm_pack_weights(desc: LayerDesc, weights: Weights, bitmap=None, stream: Opti
     """Fills the packed buffers named in `weights` (wp_*/wsp_*) from its public arrays."""
     _check(load_library().bm_pack_weights(ctypes.byref(desc), ctypes.byref(weights), _ptr(bitmap),
                                           _stream() if stream is None else stream), "bm_pack_weights")
+
+
+def bm_quantize(desc: QuantizeDesc, src, q, scale, stream: Optional[int] = None):
+    """e4m3 values and block scales of src; desc.block_rows 1 for activations, 128 for weights."""
+    _check(load_library().bm_quantize(ctypes.byref(desc), _ptr(src), _ptr(q), _ptr(scale),
+                                      _stream() if stream is None else stream), "bm_quantize")
+
+
+def bm_add_rmsnorm(desc: NormDesc, x, residual, gamma, residual_out=None, y=None, q=None, scale=None,
+                   stream: Optional[int] = None):
+    _check(load_library().bm_add_rmsnorm(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(residual_out),
+                                         _ptr(y), _ptr(q), _ptr(scale), _stream() if stream is None else stream),
+           "bm_add_rmsnorm")
+
+
+def bm_grouped_matmul(desc: ProductDesc, a, a_scale, row_map, offsets, w, w_scale, c, stream: Optional[int] = None):
+    _check(load_library().bm_grouped_matmul(ctypes.byref(desc), _ptr(a), _ptr(a_scale), _ptr(row_map), _ptr(offsets),
+                                            _ptr(w), _ptr(w_scale), _ptr(c), _stream() if stream is None else stream),
+           "bm_grouped_matmul")
+
+
+def bm_grouped_swiglu(desc: ProductDesc, a, a_scale, row_map, offsets, w_gate, gate_scale, w_up, up_scale, h, h_scale,
+                      stream: Optional[int] = None):
+    _check(load_library().bm_grouped_swiglu(ctypes.byref(desc), _ptr(a), _ptr(a_scale), _ptr(row_map), _ptr(offsets),
+                                            _ptr(w_gate), _ptr(gate_scale), _ptr(w_up), _ptr(up_scale), _ptr(h),
+                                            _ptr(h_scale), _stream() if stream is None else stream), "bm_grouped_swiglu")
+
+
+def make_quantized_weights(w_router, router_bias, w_gate, gate_scale, w_up, up_scale, w_down, down_scale, ws_gate=None,
+                           ws_gate_scale=None, ws_up=None, ws_up_scale=None, ws_down=None, ws_down_scale=None,
+                           buddy_q=None) -> QuantizedWeights:
+    return QuantizedWeights(*[_ptr(t) for t in (w_router, router_bias, w_gate, gate_scale, w_up, up_scale, w_down, down_scale,
+                                                ws_gate, ws_gate_scale, ws_up, ws_up_scale, ws_down, ws_down_scale, buddy_q)])
+
+
+def bm_workspace_bytes_quantized(desc: LayerDesc) -> int:
+    return int(load_library().bm_workspace_bytes_quantized(ctypes.byref(desc)))
+
+
+def bm_moe_forward_quantized(desc: LayerDesc, x, x_q, x_scale, weights: QuantizedWeights, bitmap, table, y, workspace,
+                             dbg: Optional[dict] = None, stream: Optional[int] = None):
+    """bm_moe_forward on 8-bit experts; x_q and x_scale as bm_add_rmsnorm writes them, or None for both.  dbg as there."""
+    d = _debug_struct(dbg)
+    _check(load_library().bm_moe_forward_quantized(ctypes.byref(desc), _ptr(x), _ptr(x_q), _ptr(x_scale), ctypes.byref(weights),
+                                                   _ptr(bitmap), _ptr(table), _ptr(y), _ptr(workspace),
+                                                   workspace.numel() * workspace.element_size(),
+                                                   ctypes.byref(d) if d is not None else None,
+                                                   _stream() if stream is None else stream), "bm_moe_forward_quantized")

@@ -4,6 +4,7 @@
 #include "bm_kernels.h"
 #include "bm_dispatch_rules.h"
 #include "bm_device_shape.h"
+#include "bm_products.h"
 
 #include <atomic>
 #include <cstdio>
@@ -259,6 +260,200 @@ int static_scratch_ptr(void **out) {
     return BM_OK;
 }
 
+// Steps 1-3 of the layer - router, gates and substitution; offsets, tile bases, row-tile table, statistics; stable
+// placement - with their arrays in the workspace.  The caller sets the scan's row-tile members (BM, mixed, largest_first).
+struct FrontEnd {
+    FrontParams fp;
+    ScanParams sp;
+    ScatterParams cp;
+    bool fuse;
+};
+
+// logits_space: where the router's logits may go if they fit (nothing is held there before the projections)
+FrontEnd plan_front(const bm_layer_desc *desc, const void *x, const void *w_router, const float *router_bias, const float *buddy_q,
+                    const uint64_t *residency_bitmap, const int32_t *buddy_table, void *ws, const Layout &L, float *logits_space,
+                    size_t logits_bytes) {
+    const int T = desc->T, K = desc->K, E = desc->E;
+    FrontEnd f{};
+    FrontParams &fp = f.fp;
+    fp.x = x; fp.wr = w_router; fp.bias = router_bias;
+    fp.T = T; fp.d = desc->d; fp.E = E; fp.K = K; fp.R = desc->R; fp.H = desc->H; fp.flags = desc->flags;
+    fp.tau = desc->tae_tau; fp.gamma = desc->margin_gamma; fp.rho = desc->rho; fp.beta = desc->dist_beta;
+    fp.q = buddy_q; fp.eta = desc->psi_eta; fp.probs_out = nullptr;
+    fp.ids = at<int32_t>(ws, L.ids); fp.w = at<float>(ws, L.w);
+    fp.bitmap = residency_bitmap; fp.table = buddy_table;
+    fp.ids2 = at<int32_t>(ws, L.ids2);
+    fp.tile_counts = at<int32_t>(ws, L.tile_counts);
+    fp.tile_stats = at<int32_t>(ws, L.tile_stats);
+    f.fuse = front_can_fuse(T, desc->dtype, desc->flags);
+    if (!f.fuse && front_wants_logits(fp, desc->dtype) && (size_t)T * E * 4 <= logits_bytes) fp.logits = logits_space;
+    fp.tile_tokens = front_tile_tokens(T, desc->dtype, f.fuse);
+
+    ScanParams &sp = f.sp;
+    sp.T = T; sp.E = E; sp.n_shared = desc->n_shared;
+    sp.n_tiles = (T + fp.tile_tokens - 1) / fp.tile_tokens;   // tiles of the front kernel (per-tile statistics)
+    sp.tile_counts = fp.tile_counts; sp.tile_base = at<int32_t>(ws, L.tile_base);
+    sp.tile_stats = fp.tile_stats;
+    sp.offsets = at<int32_t>(ws, L.offsets);
+    sp.mt_group = at<int32_t>(ws, L.mt_group); sp.mt_row0 = at<int32_t>(ws, L.mt_row0);
+    sp.n_mtiles = at<int32_t>(ws, L.n_mtiles);
+    sp.stats = at<int32_t>(ws, L.stats);
+
+    ScatterParams &cp = f.cp;
+    cp.T = T; cp.K = K; cp.E = E; cp.n_shared = desc->n_shared; cp.tile_tokens = fp.tile_tokens;
+    cp.ids = fp.ids2; cp.offsets = sp.offsets; cp.tile_base = sp.tile_base;
+    cp.perm = at<int32_t>(ws, L.perm); cp.inv_perm = at<int32_t>(ws, L.inv_perm);
+    cp.row_token = at<int32_t>(ws, L.row_token);
+    return f;
+}
+
+int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, const Layout &L, hipStream_t st) {
+    const int T = desc->T, K = desc->K, E = desc->E;
+    FrontParams fp = f.fp;
+    const ScanParams &sp = f.sp;
+    const ScatterParams &cp = f.cp;
+    int err = 0;
+    if (f.fuse) {                              // decode-sized batch: one kernel does steps 1-3
+        fp.fused = 1;
+        fp.scan = sp;
+        fp.scat = cp;
+        err |= launch_front(fp, desc->dtype, st);
+    } else if (desc->flags & BM_GATE_DIST) {
+        // the distribution gate needs every token's routing before the first substitution: route,
+        // then substitute (each workgroup derives the batch's request set itself), then count
+        FrontParams rp = fp;
+        rp.bitmap = nullptr;
+        const bool psi = (desc->flags & BM_PSI_TOKEN) != 0;
+        if (psi) rp.probs_out = at<float>(ws, L.probs);
+        err |= launch_front(rp, desc->dtype, st);
+        RemapParams mp{};
+        mp.T = T; mp.K = K; mp.E = E; mp.R = desc->R; mp.H = desc->H;
+        mp.flags = desc->flags; mp.tau = fp.tau; mp.gamma = fp.gamma; mp.rho = fp.rho; mp.beta = fp.beta;
+        mp.bitmap = fp.bitmap; mp.table = fp.table;
+        mp.q = fp.q; mp.eta = fp.eta; mp.probs = psi ? at<float>(ws, L.probs) : nullptr;
+        mp.ids_in = fp.ids; mp.ids_out = fp.ids2; mp.w = fp.w; mp.stats = sp.stats;
+        err |= launch_remap(mp, st);
+        if (!grouping_small((long long)T * K, E)) err |= launch_count(fp.ids2, T, K, E, fp.tile_tokens, fp.tile_counts, st);
+        ScanParams sq = sp;
+        sq.tile_stats = nullptr; sq.stats = nullptr;      // written by the substitution kernel
+        err |= launch_grouping(sq, cp, st);
+    } else if (sp.n_tiles == 1) {
+        fp.tail = 1;                           // a single tile: its workgroup finishes the grouping too
+        fp.scan = sp;
+        fp.scat = cp;
+        err |= launch_front(fp, desc->dtype, st);
+    } else {
+        err |= launch_front(fp, desc->dtype, st);
+        err |= launch_grouping(sp, cp, st);
+    }
+    return err;
+}
+
+// The intermediate index arrays that a caller asked for
+int copy_debug(const bm_debug_out *dbg, const FrontEnd &f, hipStream_t st) {
+    const size_t A = (size_t)f.fp.T * f.fp.K;
+    if (dbg->ids) copy_ints(f.fp.ids, dbg->ids, A, st);
+    if (dbg->ids_remapped) copy_ints(f.fp.ids2, dbg->ids_remapped, A, st);
+    if (dbg->w) copy_ints(f.fp.w, dbg->w, A, st);
+    if (dbg->offsets) copy_ints(f.sp.offsets, dbg->offsets, (size_t)f.fp.E + 1, st);
+    if (dbg->perm) copy_ints(f.cp.perm, dbg->perm, A, st);
+    if (dbg->inv_perm) copy_ints(f.cp.inv_perm, dbg->inv_perm, A, st);
+    if (dbg->stats) copy_ints(f.sp.stats, dbg->stats, 6, st);
+    return launch_status("debug copies");
+}
+
+// The five events that a caller wants recorded between the stages
+int stage_events(const bm_debug_out *dbg, hipEvent_t (&ev)[5]) {
+    for (int i = 0; i < 5; ++i) ev[i] = nullptr;
+    if (dbg && dbg->stage_events[0])
+        for (int i = 0; i < 5; ++i) {
+            if (!dbg->stage_events[i]) return BM_ERR_NULL;
+            ev[i] = static_cast<hipEvent_t>(dbg->stage_events[i]);
+        }
+    return BM_OK;
+}
+
+// ---- the layer on 8-bit weights -------------------------------------------------------------------------------------
+
+constexpr int O_F32_TOKENS = 256;    // up to this many tokens an expert's output is held in fp32 (it is small, and y one rounding more exact)
+
+// Workspace of bm_moe_forward_quantized: the front end's arrays, the 8-bit tokens, h and the experts' outputs.
+struct QuantizedLayout {
+    Layout front;
+    size_t xq, xs, h, hs, o, total;
+    bool o_f32;
+};
+
+int check_quantized_desc(const bm_layer_desc *d) {
+    int rc = check_desc(d, true);
+    if (rc) return rc;
+    if (d->dtype != BM_BF16) return BM_ERR_DTYPE;
+    if (d->d > MAX_PRODUCT_KD || d->F > MAX_PRODUCT_KD) return BM_ERR_SHAPE;
+    if ((long long)d->T * (d->K + d->n_shared) > (1ll << 30)) return BM_ERR_SHAPE;
+    return BM_OK;
+}
+
+QuantizedLayout make_quantized_layout(const bm_layer_desc *d) {
+    QuantizedLayout Q{};
+    Layout &L = Q.front;
+    const size_t A = (size_t)d->T * d->K;
+    const int tiles16 = (d->T + 15) / 16;
+    L.rows_max = (int)(A + (size_t)d->n_shared * d->T);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
+    L.ids = take(A * 4);
+    L.ids2 = take(A * 4);
+    L.w = take(A * 4);
+    L.tile_counts = take((size_t)tiles16 * d->E * 4);
+    L.tile_base = take((size_t)tiles16 * d->E * 4);
+    L.tile_stats = take((size_t)tiles16 * 16);
+    L.offsets = take((size_t)(d->E + d->n_shared + 1) * 4);
+    L.perm = take(A * 4);
+    L.inv_perm = take(A * 4);
+    L.row_token = take((size_t)L.rows_max * 4);
+    L.mt_group = take((size_t)(d->E + d->n_shared) * 4);     // one entry per live group (a tile height that no group reaches)
+    L.mt_row0 = take((size_t)(d->E + d->n_shared) * 4);
+    L.n_mtiles = take(16);
+    L.stats = take(32);
+    L.probs = take(((d->flags & BM_PSI_TOKEN) && (d->flags & BM_GATE_DIST)) ? (size_t)d->T * d->E * 4 : 0);
+    const size_t db = (d->d + SCALE_BLOCK - 1) / SCALE_BLOCK, fb = (d->F + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    Q.o_f32 = d->T <= O_F32_TOKENS;
+    Q.xq = take((size_t)d->T * d->d);
+    Q.xs = take((size_t)d->T * db * 4);
+    Q.h = take((size_t)L.rows_max * d->F);
+    Q.hs = take((size_t)L.rows_max * fb * 4);
+    // a larger batch of the layer needs no less: its workspace serves the smaller ones too
+    const size_t most_f32 = (size_t)O_F32_TOKENS * (d->K + d->n_shared) * d->d * 4, o_bytes = (size_t)L.rows_max * d->d * (Q.o_f32 ? 4 : 2);
+    Q.o = take(!Q.o_f32 && o_bytes < most_f32 ? most_f32 : o_bytes);
+    Q.total = off;
+    return Q;
+}
+
+// ---- argument checks of the 8-bit operators ----
+
+bool off16(const void *p) { return !aligned16(p); }
+
+int check_product(const bm_product_desc *d, const void *a, const float *a_scale, const int32_t *row_map, const int32_t *offsets) {
+    if (!d) return BM_ERR_NULL;
+    if (d->rows < 0 || d->rows > (1 << 30) || d->a_rows < 0 || d->N <= 0 || d->Kd <= 0 || d->E <= 0 || d->E > BM_MAX_E || d->K <= 0)
+        return BM_ERR_SHAPE;
+    if (d->N % 32 || d->Kd % 32 || d->Kd > MAX_PRODUCT_KD || d->N > (1 << 20)) return BM_ERR_SHAPE;
+    if (!offsets && d->E > 1) return BM_ERR_NULL;
+    if (d->rows > 0 && (d->a_rows == 0 || (!row_map && d->a_rows < d->rows))) return BM_ERR_SHAPE;
+    if (!product_grid_ok(d->rows, d->N, d->E)) return BM_ERR_SHAPE;
+    if (d->rows > 0 && (!a || !a_scale)) return BM_ERR_NULL;
+    return BM_OK;
+}
+
+ProductParams product_params(const bm_product_desc *d, const void *a, const float *a_scale, const int32_t *row_map, const int32_t *offsets) {
+    ProductParams p{};
+    p.a = static_cast<const uint8_t *>(a); p.a_scale = a_scale;
+    p.row_map = row_map; p.map_div = d->K; p.a_rows = d->a_rows;
+    p.offsets = offsets; p.E = p.n_groups = d->E;
+    p.rows = d->rows; p.N = d->N; p.Kd = d->Kd;
+    return p;
+}
+
 }  // namespace
 
 extern "C" {
@@ -279,6 +474,7 @@ const char *bm_strerror(int status) {
         case BM_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case BM_ERR_BAD_TABLE: return "buddy table entry out of range or equal to its row";
         case BM_ERR_HIP: return "kernel launch failed";
+        case BM_ERR_ALIGN: return "array off its required boundary";
         default: return "unknown status";
     }
 }
@@ -476,37 +672,20 @@ int bm_moe_forward(const bm_layer_desc *desc, const void *x, const bm_weights *w
     int err = 0;
     (void)hipGetLastError();   // errors left by earlier, unrelated HIP calls are not ours
 
-    hipEvent_t ev[5] = {nullptr, nullptr, nullptr, nullptr, nullptr};
-    if (dbg && dbg->stage_events[0])
-        for (int i = 0; i < 5; ++i) {
-            if (!dbg->stage_events[i]) return BM_ERR_NULL;
-            ev[i] = static_cast<hipEvent_t>(dbg->stage_events[i]);
-        }
+    hipEvent_t ev[5];
+    rc = stage_events(dbg, ev);
+    if (rc) return rc;
     auto mark = [&](int i) { if (ev[i]) err |= (hipEventRecord(ev[i], st) != hipSuccess); };
 
-    // 1. router, gates, substitution, per-tile histograms
+    // 1.-3. router, gates, substitution, grouping
     mark(0);
-    FrontParams fp{};
-    fp.x = x; fp.wr = wt->w_router; fp.bias = wt->router_bias;
-    fp.T = T; fp.d = desc->d; fp.E = E; fp.K = K; fp.R = desc->R; fp.H = desc->H; fp.flags = desc->flags;
-    fp.tau = desc->tae_tau; fp.gamma = desc->margin_gamma; fp.rho = desc->rho; fp.beta = desc->dist_beta;
-    fp.q = wt->buddy_q; fp.eta = desc->psi_eta; fp.probs_out = nullptr;
-    fp.ids = at<int32_t>(ws, L.ids); fp.w = at<float>(ws, L.w);
-    fp.bitmap = residency_bitmap; fp.table = buddy_table;
-    fp.ids2 = at<int32_t>(ws, L.ids2);
-    fp.tile_counts = at<int32_t>(ws, L.tile_counts);
-    fp.tile_stats = at<int32_t>(ws, L.tile_stats);
-    const bool fuse = front_can_fuse(T, desc->dtype, desc->flags);
     // the logits borrow the space of h, which nothing holds before the gate/up projection
-    if (!fuse && front_wants_logits(fp, desc->dtype) && (size_t)T * E * 4 <= (size_t)L.rows_max * desc->F * (bf16 ? 2 : 4))
-        fp.logits = at<float>(ws, L.h);
-    fp.tile_tokens = front_tile_tokens(T, desc->dtype, fuse);
-
-    // 2. offsets, tile bases, row-tile table, statistics
-    ScanParams sp{};
+    FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
+                             at<float>(ws, L.h), (size_t)L.rows_max * desc->F * (bf16 ? 2 : 4));
+    const FrontParams &fp = fe.fp;
+    ScanParams &sp = fe.sp;
+    const ScatterParams &cp = fe.cp;
     const bool skinny = L.skinny;
-    sp.T = T; sp.E = E; sp.n_shared = desc->n_shared;
-    sp.n_tiles = (T + fp.tile_tokens - 1) / fp.tile_tokens;   // tiles of the front kernel (per-tile statistics)
     const bool persistent = !skinny && bf16 && persistent_device();
     const bool per_group = skinny || !bf16;              // decode and fp32 projections: one table entry per live group
     const int mode_gu = per_group ? (1 << 30) : tile_mode(desc, false, persistent);
@@ -521,52 +700,7 @@ int bm_moe_forward(const bm_layer_desc *desc, const void *x, const bm_weights *w
         sp.n_mtiles_s = at<int32_t>(ws, L.n_mtiles_s);
     }
     sp.largest_first = per_group ? 1 : 0;
-    sp.tile_counts = fp.tile_counts; sp.tile_base = at<int32_t>(ws, L.tile_base);
-    sp.tile_stats = fp.tile_stats;
-    sp.offsets = at<int32_t>(ws, L.offsets);
-    sp.mt_group = at<int32_t>(ws, L.mt_group); sp.mt_row0 = at<int32_t>(ws, L.mt_row0);
-    sp.n_mtiles = at<int32_t>(ws, L.n_mtiles);
-    sp.stats = at<int32_t>(ws, L.stats);
-
-    // 3. stable placement
-    ScatterParams cp{};
-    cp.T = T; cp.K = K; cp.E = E; cp.n_shared = desc->n_shared; cp.tile_tokens = fp.tile_tokens;
-    cp.ids = fp.ids2; cp.offsets = sp.offsets; cp.tile_base = sp.tile_base;
-    cp.perm = at<int32_t>(ws, L.perm); cp.inv_perm = at<int32_t>(ws, L.inv_perm);
-    cp.row_token = at<int32_t>(ws, L.row_token);
-    if (fuse) {                                // decode-sized batch: one kernel does steps 1-3
-        fp.fused = 1;
-        fp.scan = sp;
-        fp.scat = cp;
-        err |= launch_front(fp, desc->dtype, st);
-    } else if (desc->flags & BM_GATE_DIST) {
-        // the distribution gate needs every token's routing before the first substitution: route,
-        // then substitute (each workgroup derives the batch's request set itself), then count
-        FrontParams rp = fp;
-        rp.bitmap = nullptr;
-        const bool psi = (desc->flags & BM_PSI_TOKEN) != 0;
-        if (psi) rp.probs_out = at<float>(ws, L.probs);
-        err |= launch_front(rp, desc->dtype, st);
-        RemapParams mp{};
-        mp.T = T; mp.K = K; mp.E = E; mp.R = desc->R; mp.H = desc->H;
-        mp.flags = desc->flags; mp.tau = fp.tau; mp.gamma = fp.gamma; mp.rho = fp.rho; mp.beta = fp.beta;
-        mp.bitmap = residency_bitmap; mp.table = buddy_table;
-        mp.q = fp.q; mp.eta = fp.eta; mp.probs = psi ? at<float>(ws, L.probs) : nullptr;
-        mp.ids_in = fp.ids; mp.ids_out = fp.ids2; mp.w = fp.w; mp.stats = sp.stats;
-        err |= launch_remap(mp, st);
-        if (!grouping_small((long long)T * K, E)) err |= launch_count(fp.ids2, T, K, E, fp.tile_tokens, fp.tile_counts, st);
-        ScanParams sq = sp;
-        sq.tile_stats = nullptr; sq.stats = nullptr;      // written by the substitution kernel
-        err |= launch_grouping(sq, cp, st);
-    } else if (sp.n_tiles == 1) {
-        fp.tail = 1;                           // a single tile: its workgroup finishes the grouping too
-        fp.scan = sp;
-        fp.scat = cp;
-        err |= launch_front(fp, desc->dtype, st);
-    } else {
-        err |= launch_front(fp, desc->dtype, st);
-        err |= launch_grouping(sp, cp, st);
-    }
+    err |= launch_front_end(desc, fe, ws, L, st);
     mark(1);
 
     // 4. gate/up projection + SwiGLU, 5. down projection
@@ -646,17 +780,147 @@ int bm_moe_forward(const bm_layer_desc *desc, const void *x, const bm_weights *w
     if (!combined) err |= launch_combine(mp, bf16 && !skinny, st);
     mark(4);
 
-    if (dbg) {
-        const size_t A = (size_t)T * K;
-        if (dbg->ids) copy_ints(fp.ids, dbg->ids, A, st);
-        if (dbg->ids_remapped) copy_ints(fp.ids2, dbg->ids_remapped, A, st);
-        if (dbg->w) copy_ints(fp.w, dbg->w, A, st);
-        if (dbg->offsets) copy_ints(sp.offsets, dbg->offsets, (size_t)E + 1, st);
-        if (dbg->perm) copy_ints(cp.perm, dbg->perm, A, st);
-        if (dbg->inv_perm) copy_ints(cp.inv_perm, dbg->inv_perm, A, st);
-        if (dbg->stats) copy_ints(sp.stats, dbg->stats, 6, st);
-        err |= launch_status("debug copies");
+    if (dbg) err |= copy_debug(dbg, fe, st);
+    return err ? BM_ERR_HIP : BM_OK;
+}
+
+int bm_quantize(const bm_quantize_desc *d, const void *src, void *q, float *scale, void *stream) {
+    if (!d) return BM_ERR_NULL;
+    if (d->dtype != BM_F32 && d->dtype != BM_BF16) return BM_ERR_DTYPE;
+    if (d->n < 0 || d->rows < 0 || d->cols < 0 || (d->block_rows != 1 && d->block_rows != SCALE_BLOCK)) return BM_ERR_SHAPE;
+    if (d->n == 0 || d->rows == 0 || d->cols == 0) return BM_OK;
+    if (!quantize_grid_ok(d->n, d->rows, d->cols, d->block_rows != 1)) return BM_ERR_SHAPE;
+    if (!src || !q || !scale) return BM_ERR_NULL;
+    (void)hipGetLastError();
+    return launch_quantize(src, d->dtype == BM_F32, static_cast<uint8_t *>(q), scale, d->n, d->rows, d->cols, d->block_rows != 1,
+                           static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
+}
+
+int bm_add_rmsnorm(const bm_norm_desc *d, const void *x, const void *residual, const void *gamma, void *residual_out, void *y,
+                   void *q, float *scale, void *stream) {
+    if (!d) return BM_ERR_NULL;
+    if (d->dtype != BM_F32 && d->dtype != BM_BF16) return BM_ERR_DTYPE;
+    if (d->T < 0 || d->d <= 0 || d->d > MAX_NORM_D || !(d->eps >= 0.0f) || d->eps > 3.0e38f) return BM_ERR_SHAPE;
+    if (d->T == 0) return BM_OK;
+    if (!x || !gamma || (q && !scale) || (!residual_out && !y && !q)) return BM_ERR_NULL;
+    if (y && y == residual_out) return BM_ERR_SHAPE;
+    (void)hipGetLastError();
+    NormParams p{};
+    p.x = x; p.residual = residual; p.gamma = gamma;
+    p.residual_out = residual_out; p.y = y; p.q = static_cast<uint8_t *>(q); p.scale = scale;
+    p.T = d->T; p.d = d->d; p.eps = d->eps;
+    return launch_add_rmsnorm(p, d->dtype == BM_F32, static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
+}
+
+int bm_grouped_matmul(const bm_product_desc *d, const void *a, const float *a_scale, const int32_t *row_map, const int32_t *offsets,
+                      const void *w, const float *w_scale, void *c, void *stream) {
+    int rc = check_product(d, a, a_scale, row_map, offsets);
+    if (rc) return rc;
+    if (d->dtype != BM_F32 && d->dtype != BM_BF16) return BM_ERR_DTYPE;
+    if (d->rows == 0) return BM_OK;
+    if (!w || !w_scale || !c) return BM_ERR_NULL;
+    if (off16(a) || off16(w) || off16(c)) return BM_ERR_ALIGN;
+    (void)hipGetLastError();
+    ProductParams p = product_params(d, a, a_scale, row_map, offsets);
+    p.b0 = static_cast<const uint8_t *>(w); p.bs0 = w_scale;
+    p.c = c; p.c_f32 = d->dtype == BM_F32;
+    return launch_product(p, static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
+}
+
+int bm_grouped_swiglu(const bm_product_desc *d, const void *a, const float *a_scale, const int32_t *row_map, const int32_t *offsets,
+                      const void *w_gate, const float *gate_scale, const void *w_up, const float *up_scale, void *h, float *h_scale,
+                      void *stream) {
+    int rc = check_product(d, a, a_scale, row_map, offsets);
+    if (rc) return rc;
+    if (d->rows == 0) return BM_OK;
+    if (!w_gate || !gate_scale || !w_up || !up_scale || !h || !h_scale) return BM_ERR_NULL;
+    if (off16(a) || off16(w_gate) || off16(w_up) || off16(h)) return BM_ERR_ALIGN;
+    (void)hipGetLastError();
+    ProductParams p = product_params(d, a, a_scale, row_map, offsets);
+    p.b0 = static_cast<const uint8_t *>(w_gate); p.bs0 = gate_scale;
+    p.b1 = static_cast<const uint8_t *>(w_up); p.bs1 = up_scale;
+    p.c = h; p.c_scale = h_scale;
+    return launch_swiglu(p, static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
+}
+
+size_t bm_workspace_bytes_quantized(const bm_layer_desc *desc) {
+    if (check_quantized_desc(desc) != BM_OK) return 0;
+    return make_quantized_layout(desc).total;
+}
+
+int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale,
+                             const bm_quantized_weights *wt, const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y,
+                             void *workspace, size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
+    int rc = check_quantized_desc(desc);
+    if (rc) return rc;
+    rc = check_remap_desc(desc);
+    if (rc) return rc;
+    const int T = desc->T, K = desc->K, E = desc->E, G = E + desc->n_shared;
+    if (T == 0) return BM_OK;
+    if (!product_grid_ok((long long)T * (K + desc->n_shared), desc->d > desc->F ? desc->d : desc->F, G)) return BM_ERR_SHAPE;
+    if (!x || !wt || !residency_bitmap || !y || (!buddy_table && desc->R > 0) || !x_q != !x_scale) return BM_ERR_NULL;
+    if (!wt->w_router || !wt->w_gate || !wt->gate_scale || !wt->w_up || !wt->up_scale || !wt->w_down || !wt->down_scale) return BM_ERR_NULL;
+    if (desc->n_shared > 0 && (!wt->ws_gate || !wt->ws_gate_scale || !wt->ws_up || !wt->ws_up_scale || !wt->ws_down || !wt->ws_down_scale))
+        return BM_ERR_NULL;
+    if ((desc->flags & BM_PSI_TOKEN) && !wt->buddy_q) return BM_ERR_NULL;
+    if (off16(x) || off16(x_q) || off16(wt->w_gate) || off16(wt->w_up) || off16(wt->w_down) || off16(wt->ws_gate) ||
+        off16(wt->ws_up) || off16(wt->ws_down)) return BM_ERR_ALIGN;
+    const QuantizedLayout Q = make_quantized_layout(desc);
+    const Layout &L = Q.front;
+    void *ws = workspace;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) % ALIGN) || workspace_bytes < Q.total) return BM_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipEvent_t ev[5];
+    rc = stage_events(dbg, ev);
+    if (rc) return rc;
+    int err = 0;
+    (void)hipGetLastError();
+    auto mark = [&](int i) { if (ev[i]) err |= (hipEventRecord(ev[i], st) != hipSuccess); };
+
+    mark(0);
+    // the logits borrow the space of o, which nothing holds before the down projection
+    FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
+                             at<float>(ws, Q.o), (size_t)L.rows_max * desc->d * (Q.o_f32 ? 4 : 2));
+    fe.sp.BM = 1 << 30;                       // the products find their tiles from the offsets: the table is not read
+    err |= launch_front_end(desc, fe, ws, L, st);
+    if (!x_q) {
+        err |= launch_quantize(x, false, at<uint8_t>(ws, Q.xq), at<float>(ws, Q.xs), 1, T, desc->d, false, st);
+        x_q = at<uint8_t>(ws, Q.xq);
+        x_scale = at<float>(ws, Q.xs);
     }
+    mark(1);
+
+    ProductParams gp{};
+    gp.a = static_cast<const uint8_t *>(x_q); gp.a_scale = x_scale;
+    gp.row_map = fe.cp.row_token; gp.map_div = 1; gp.a_rows = T;
+    gp.b0 = static_cast<const uint8_t *>(wt->w_gate); gp.bs0 = wt->gate_scale;
+    gp.b1 = static_cast<const uint8_t *>(wt->w_up); gp.bs1 = wt->up_scale;
+    gp.sb0 = static_cast<const uint8_t *>(wt->ws_gate); gp.sbs0 = wt->ws_gate_scale;
+    gp.sb1 = static_cast<const uint8_t *>(wt->ws_up); gp.sbs1 = wt->ws_up_scale;
+    gp.offsets = fe.sp.offsets; gp.E = E; gp.n_groups = G;
+    gp.rows = L.rows_max; gp.N = desc->F; gp.Kd = desc->d;
+    gp.c = at<void>(ws, Q.h); gp.c_scale = at<float>(ws, Q.hs);
+    err |= launch_swiglu(gp, st);
+    mark(2);
+    ProductParams dp = gp;
+    dp.a = at<uint8_t>(ws, Q.h); dp.a_scale = at<float>(ws, Q.hs);
+    dp.row_map = nullptr; dp.a_rows = L.rows_max;
+    dp.b0 = static_cast<const uint8_t *>(wt->w_down); dp.bs0 = wt->down_scale;
+    dp.b1 = nullptr; dp.bs1 = nullptr; dp.sb1 = nullptr; dp.sbs1 = nullptr;
+    dp.sb0 = static_cast<const uint8_t *>(wt->ws_down); dp.sbs0 = wt->ws_down_scale;
+    dp.N = desc->d; dp.Kd = desc->F;
+    dp.c = at<void>(ws, Q.o); dp.c_scale = nullptr; dp.c_f32 = Q.o_f32;
+    err |= launch_product(dp, st);
+    mark(3);
+
+    CombineParams mp{};
+    mp.T = T; mp.d = desc->d; mp.K = K; mp.E = E; mp.n_shared = desc->n_shared;
+    mp.ksplit = 1; mp.slice_stride = 0;
+    mp.o = dp.c; mp.w = fe.fp.w; mp.inv_perm = fe.cp.inv_perm; mp.offsets = fe.sp.offsets;
+    mp.y = y; mp.y_f32 = (desc->flags & BM_Y_F32) ? 1 : 0;
+    err |= launch_combine(mp, !Q.o_f32, st);
+    mark(4);
+    if (dbg) err |= copy_debug(dbg, fe, st);
     return err ? BM_ERR_HIP : BM_OK;
 }
 

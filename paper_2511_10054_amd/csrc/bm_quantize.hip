@@ -1,0 +1,256 @@
+// Quantization to 8 bits (e4m3: sign, four exponent and three mantissa bits, no infinities) with one 32-bit scale for each block of 128
+// values, alone (bm_quantize) and behind the residual's addition and the root-mean-square norm (bm_add_rmsnorm).
+//
+// Of a block with largest magnitude m:  s = max(m / 448, 2^-126),  q = e4m3(x / s), every rounding to nearest even and
+// both quotients rounded to 32 bits.  s keeps q within e4m3's +-448 and 1 / s finite.  A block that holds an infinity or
+// a NaN gets s = NaN and NaN throughout: what it stands for is no number either.
+#include "bm_quantize.h"
+
+namespace bm {
+
+namespace {
+
+// Largest magnitude over the 16 lanes that share a block, as the bits of a non-negative float: for those the order of the
+// numbers is the order of the bits, and a NaN is above everything.
+__device__ __forceinline__ uint32_t row16_max_u32(uint32_t v) {
+#define BM_DPP_MAX16(ctrl_)                                                                             \
+    {                                                                                                   \
+        const uint32_t o_ = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, ctrl_, 0xF, 0xF, false); \
+        v = o_ > v ? o_ : v;                                                                            \
+    }
+    BM_DPP_MAX16(0xB1)     // quad_perm [1, 0, 3, 2]
+    BM_DPP_MAX16(0x4E)     // quad_perm [2, 3, 0, 1]
+    BM_DPP_MAX16(0x141)    // row_half_mirror
+    BM_DPP_MAX16(0x140)    // row_mirror
+#undef BM_DPP_MAX16
+    return v;
+}
+
+__device__ __forceinline__ uint32_t max_bits(const float (&v)[8], uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu);
+    return m;
+}
+
+// Eight consecutive values from p, zeros from the n-th on.  ALIGNED: p lies on a 16-byte boundary and n >= 8.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void load8(const T *p, int n, float (&v)[8]) {
+    if (ALIGNED && sizeof(T) == 2) {
+        const u32x4 u = ldg128(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = bf16_to_f32((uint16_t)(u[i] & 0xffffu));
+            v[2 * i + 1] = bf16_to_f32((uint16_t)(u[i] >> 16));
+        }
+    } else if (ALIGNED) {
+        const f32x4 a = *(const BM_GLOBAL f32x4 *)p, b = *((const BM_GLOBAL f32x4 *)p + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.0f;
+            if (i < n) {
+                if (sizeof(T) == 2) v[i] = bf16_to_f32(*(const BM_GLOBAL uint16_t *)(const void *)(p + i));
+                else v[i] = ldg_f32(p + i);
+            }
+        }
+    }
+}
+
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
+    if (ALIGNED && sizeof(T) == 2) {
+        u32x4 u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        stg128(p, u);
+    } else if (ALIGNED) {
+        f32x4 a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { a[i] = v[i]; b[i] = v[4 + i]; }
+        *(BM_GLOBAL f32x4 *)p = a;
+        *((BM_GLOBAL f32x4 *)p + 1) = b;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) {
+                if (sizeof(T) == 2) stg16(p + i, f32_to_bf16(v[i]));
+                else *(BM_GLOBAL float *)(void *)(p + i) = v[i];
+            }
+    }
+}
+
+template <bool ALIGNED>
+__device__ __forceinline__ void store_q8(uint8_t *p, int n, const float (&v)[8], float s, float inv) {
+    const uint32_t lo = e4m3x4(quotient(v[0], s, inv), quotient(v[1], s, inv), quotient(v[2], s, inv), quotient(v[3], s, inv));
+    const uint32_t hi = e4m3x4(quotient(v[4], s, inv), quotient(v[5], s, inv), quotient(v[6], s, inv), quotient(v[7], s, inv));
+    if (ALIGNED) {
+        const u32x2 u = {lo, hi};
+        *(BM_GLOBAL u32x2 *)p = u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) *(BM_GLOBAL uint8_t *)(p + i) = (uint8_t)((i < 4 ? lo >> (8 * i) : hi >> (8 * (i - 4))) & 0xffu);
+    }
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------------------------------------------------------------
+// A scale for each 128 values of a row: 16 lanes of eight values each hold a block.
+// ---------------------------------------------------------------------------------------------------------------------
+template <bool ALIGNED, typename T>
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const T *src, uint8_t *q, float *scale, long long n_rows, int cols, int kb) {
+    const long long blk = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const long long row = blk / kb;
+    const int j = (int)(blk - row * kb) * SCALE_BLOCK + (threadIdx.x & 15) * 8;
+    const bool in = row < n_rows && j < cols;
+    float v[8] = {};
+    const long long at = row * cols + j;
+    if (in) load8<ALIGNED>(src + at, cols - j, v);
+    const uint32_t m = row16_max_u32(max_bits(v, 0));
+    if (!in) return;
+    const float s = block_scale(m), inv = 1.0f / s;
+    store_q8<ALIGNED>(q + at, cols - j, v, s, inv);
+    if ((threadIdx.x & 15) == 0) scale[blk] = s;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// A scale for each 128 x 128 block of a matrix: one workgroup a block, its 16384 values in registers between the
+// search for the largest and the conversion.
+// ---------------------------------------------------------------------------------------------------------------------
+template <bool ALIGNED, typename T>
+__global__ void __launch_bounds__(256) quantize_blocks_kernel(const T *src, uint8_t *q, float *scale, int rows, int cols) {
+    __shared__ uint32_t s_max[4];
+    const int tid = threadIdx.x;
+    const int j = blockIdx.x * SCALE_BLOCK + (tid & 15) * 8, r0 = blockIdx.y * SCALE_BLOCK + (tid >> 4);
+    const size_t base = (size_t)blockIdx.z * rows * cols;
+    float v[8][8];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        if (r < rows && j < cols) load8<ALIGNED>(src + base + (size_t)r * cols + j, cols - j, v[i]);
+        else
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[i][u] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max_bits(v[i], m);
+    m = wave_max_u32(m);
+    if ((tid & 63) == 0) s_max[tid >> 6] = m;
+    __syncthreads();
+    m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
+    const float s = block_scale(m), inv = 1.0f / s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 16 * i;
+        if (r < rows && j < cols) store_q8<ALIGNED>(q + base + (size_t)r * cols + j, cols - j, v[i], s, inv);
+    }
+    if (tid == 0) scale[((size_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x] = s;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// r = x + residual, n = r / sqrt(mean(r^2) + eps) * gamma, in 32 bits; r and n are rounded once where they are written,
+// n's 8-bit form is made from the 32-bit values.  One workgroup a row, which stays in registers (NIT pieces of eight
+// values a thread) between the sum and the outputs: every input is read once.
+// ---------------------------------------------------------------------------------------------------------------------
+template <bool ALIGNED, typename T, int NIT>
+__global__ void __launch_bounds__(1024) add_rmsnorm_kernel(NormParams p) {
+    __shared__ float s_sum[16];
+    const int tid = threadIdx.x, nt = blockDim.x, d = p.d;
+    const size_t at = (size_t)blockIdx.x * d;
+    const T *x = static_cast<const T *>(p.x) + at, *res = p.residual ? static_cast<const T *>(p.residual) + at : nullptr;
+    const T *gamma = static_cast<const T *>(p.gamma);
+    float v[NIT][8], g[NIT][8];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) {
+        const int j = (i * nt + tid) * 8;
+        float r[8] = {};
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[i][u] = g[i][u] = 0.0f;
+        if (j < d) {
+            load8<ALIGNED>(x + j, d - j, v[i]);
+            if (res) load8<ALIGNED>(res + j, d - j, r);
+            load8<ALIGNED>(gamma + j, d - j, g[i]);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            v[i][u] += r[u];
+            sum = fmaf(v[i][u], v[i][u], sum);
+        }
+    }
+    sum = wave_sum(sum);
+    if (nt > WAVE) {
+        if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
+        __syncthreads();
+        sum = 0.0f;
+        for (int w = 0; w < nt / WAVE; ++w) sum += s_sum[w];
+    }
+    const float rs = 1.0f / sqrtf(sum / (float)d + p.eps);
+    const int kb = (d + SCALE_BLOCK - 1) / SCALE_BLOCK;
+#pragma unroll
+    for (int i = 0; i < NIT; ++i) {
+        const int j = (i * nt + tid) * 8;
+        if (p.residual_out && j < d) store8<ALIGNED>(static_cast<T *>(p.residual_out) + at + j, d - j, v[i]);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[i][u] = v[i][u] * rs * g[i][u];
+        if (p.y && j < d) store8<ALIGNED>(static_cast<T *>(p.y) + at + j, d - j, v[i]);
+        if (p.q) {
+            // lanes past the row's end hold gamma = 0 and may have 0 * infinity there: they are left out
+            const uint32_t m = row16_max_u32(j < d ? max_bits(v[i], 0) : 0u);
+            if (j < d) {
+                const float s = block_scale(m), inv = 1.0f / s;
+                store_q8<ALIGNED>(p.q + at + j, d - j, v[i], s, inv);
+                if ((tid & 15) == 0) p.scale[(size_t)blockIdx.x * kb + j / SCALE_BLOCK] = s;
+            }
+        }
+    }
+}
+
+template <typename T>
+static void launch_norm_t(const NormParams &p, hipStream_t st) {
+    const bool al = p.d % 8 == 0 && aligned16(p.x) && aligned16(p.residual) && aligned16(p.gamma) && aligned16(p.residual_out) &&
+                    aligned16(p.y) && ((uintptr_t)p.q & 7) == 0;
+    const int pieces = (p.d + 7) / 8;
+    int nt = (pieces + WAVE - 1) / WAVE * WAVE;
+    if (nt > 1024) nt = 1024;
+    const bool two = pieces > nt;
+    if (al && !two) hipLaunchKernelGGL((add_rmsnorm_kernel<true, T, 1>), dim3(p.T), dim3(nt), 0, st, p);
+    else if (al) hipLaunchKernelGGL((add_rmsnorm_kernel<true, T, 2>), dim3(p.T), dim3(nt), 0, st, p);
+    else if (!two) hipLaunchKernelGGL((add_rmsnorm_kernel<false, T, 1>), dim3(p.T), dim3(nt), 0, st, p);
+    else hipLaunchKernelGGL((add_rmsnorm_kernel<false, T, 2>), dim3(p.T), dim3(nt), 0, st, p);
+}
+
+int launch_add_rmsnorm(const NormParams &p, bool f32, hipStream_t st) {
+    if (f32) launch_norm_t<float>(p, st);
+    else launch_norm_t<uint16_t>(p, st);
+    return launch_status(__func__);
+}
+
+template <typename T>
+static void launch_quantize_t(const void *src, uint8_t *q, float *scale, int n, int rows, int cols, bool blocks, hipStream_t st) {
+    const bool al = cols % 8 == 0 && aligned16(src) && ((uintptr_t)q & 7) == 0;
+    const int kb = (cols + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    const T *s = static_cast<const T *>(src);
+    if (blocks) {
+        const dim3 grid(kb, (rows + SCALE_BLOCK - 1) / SCALE_BLOCK, n);
+        if (al) hipLaunchKernelGGL((quantize_blocks_kernel<true, T>), grid, dim3(256), 0, st, s, q, scale, rows, cols);
+        else hipLaunchKernelGGL((quantize_blocks_kernel<false, T>), grid, dim3(256), 0, st, s, q, scale, rows, cols);
+    } else {
+        const long long n_rows = (long long)n * rows;
+        const dim3 grid((unsigned)((n_rows * kb + 15) / 16));
+        if (al) hipLaunchKernelGGL((quantize_rows_kernel<true, T>), grid, dim3(256), 0, st, s, q, scale, n_rows, cols, kb);
+        else hipLaunchKernelGGL((quantize_rows_kernel<false, T>), grid, dim3(256), 0, st, s, q, scale, n_rows, cols, kb);
+    }
+}
+
+int launch_quantize(const void *src, bool f32, uint8_t *q, float *scale, int n, int rows, int cols, bool blocks, hipStream_t st) {
+    if (f32) launch_quantize_t<float>(src, q, scale, n, rows, cols, blocks, st);
+    else launch_quantize_t<uint16_t>(src, q, scale, n, rows, cols, blocks, st);
+    return launch_status(__func__);
+}
+
+}  // namespace bm

@@ -1,0 +1,153 @@
+"""The 8-bit operators' entry points on the host: struct layouts, sizes, and what they refuse before anything is launched
+(CPU only)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+import paper_2511_10054_amd as bm
+
+HDR = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+ONE = ctypes.c_void_p(256)       # non-null and aligned, never dereferenced on these paths
+ODD = ctypes.c_void_p(264)
+NULL, SHAPE, DTYPE, WORKSPACE, ALIGN = -1, -2, -3, -4, -7
+
+
+def test_struct_layouts_match_header(tmp_path):
+    structs = {"bm_quantize_desc": bm.QuantizeDesc, "bm_norm_desc": bm.NormDesc, "bm_product_desc": bm.ProductDesc,
+               "bm_quantized_weights": bm.QuantizedWeights}
+    lines = []
+    for name, cls in structs.items():
+        lines.append(f'printf("{name} %zu\\n", sizeof({name}));')
+        lines += [f'printf("{name}.{f[0]} %zu\\n", offsetof({name}, {f[0]}));' for f in cls._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "buddymoe.h"\nint main(void){' + "".join(lines) + "return 0;}\n")
+    subprocess.run(["gcc", "-I", HDR, "-o", str(tmp_path / "layout"), str(src)], check=True)
+    got = dict(l.split() for l in subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout.splitlines())
+    for name, cls in structs.items():
+        assert int(got[name]) == ctypes.sizeof(cls)
+        for f in cls._fields_:
+            assert int(got[f"{name}.{f[0]}"]) == getattr(cls, f[0]).offset
+
+
+def test_status_of_misaligned_arrays_has_a_text():
+    assert bm.bm_strerror(ALIGN) not in ("ok", "unknown status")
+
+
+@pytest.mark.parametrize("over,args,want", [
+    (dict(), (ONE, ONE, None), NULL), (dict(), (None, ONE, ONE), NULL), (dict(), (ONE, None, ONE), NULL),
+    (dict(dtype=7), (ONE, ONE, ONE), DTYPE), (dict(block_rows=64), (ONE, ONE, ONE), SHAPE), (dict(rows=-1), (ONE, ONE, ONE), SHAPE),
+    (dict(n=70000, block_rows=128), (ONE, ONE, ONE), SHAPE), (dict(n=1 << 20, rows=1 << 20, cols=1 << 20), (ONE, ONE, ONE), SHAPE),
+    (dict(rows=0), (None, None, None), 0), (dict(cols=0), (None, None, None), 0), (dict(n=0), (None, None, None), 0),
+])
+def test_quantize_refusals(over, args, want):
+    d = bm.QuantizeDesc(**dict(dict(n=1, rows=16, cols=64, block_rows=1, dtype=bm.BM_BF16), **over))
+    assert bm.load_library().bm_quantize(ctypes.byref(d), *args, None) == want
+    assert bm.load_library().bm_quantize(None, *args, None) == NULL
+
+
+@pytest.mark.parametrize("over,args,want", [
+    # x, residual, gamma, residual_out, y, q, scale
+    (dict(), (None, ONE, ONE, ONE, ODD, ONE, ONE), NULL), (dict(), (ONE, ONE, None, ONE, ODD, ONE, ONE), NULL),
+    (dict(), (ONE, ONE, ONE, None, None, None, None), NULL), (dict(), (ONE, ONE, ONE, None, None, ONE, None), NULL),
+    (dict(), (ONE, ONE, ONE, ONE, ONE, None, None), SHAPE), (dict(d=16385), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE),
+    (dict(d=0), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE), (dict(T=-1), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE),
+    (dict(eps=-1.0), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE), (dict(eps=float("nan")), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE),
+    (dict(eps=float("inf")), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE), (dict(dtype=3), (ONE,) * 4 + (ODD, ONE, ONE), DTYPE),
+    (dict(T=0), (None,) * 7, 0),
+])
+def test_norm_refusals(over, args, want):
+    d = bm.NormDesc(**dict(dict(T=4, d=64, dtype=bm.BM_F32, eps=1e-6), **over))
+    assert bm.load_library().bm_add_rmsnorm(ctypes.byref(d), *args, None) == want
+    assert bm.load_library().bm_add_rmsnorm(None, *args, None) == NULL
+
+
+PRODUCT = [
+    (dict(N=48), SHAPE), (dict(Kd=48), SHAPE), (dict(N=0), SHAPE), (dict(Kd=32800), SHAPE), (dict(E=0), SHAPE), (dict(E=257), SHAPE),
+    (dict(K=0), SHAPE), (dict(rows=-1), SHAPE), (dict(rows=(1 << 30) + 1), SHAPE), (dict(a_rows=0), SHAPE), (dict(N=1 << 21), SHAPE),
+    (dict(rows=1 << 30, a_rows=1 << 30, N=1 << 20), SHAPE),
+]
+
+
+def _product(**over):
+    return bm.ProductDesc(**dict(dict(rows=8, a_rows=8, N=64, Kd=64, E=4, K=1, dtype=bm.BM_BF16), **over))
+
+
+@pytest.mark.parametrize("over,want", PRODUCT + [(dict(dtype=2), DTYPE), (dict(rows=0), 0)])
+def test_matmul_refuses_shapes(over, want):
+    # a, a_scale, row_map, offsets, w, w_scale, c
+    assert bm.load_library().bm_grouped_matmul(ctypes.byref(_product(**over)), *(ONE,) * 7, None) == want
+
+
+@pytest.mark.parametrize("over,want", PRODUCT + [(dict(rows=0), 0)])
+def test_swiglu_refuses_shapes(over, want):
+    assert bm.load_library().bm_grouped_swiglu(ctypes.byref(_product(**over)), *(ONE,) * 10, None) == want
+
+
+def test_products_refuse_pointers():
+    lib = bm.load_library()
+    d = ctypes.byref(_product())
+
+    def but(n, i, v):
+        return [v if j == i else ONE for j in range(n)]
+
+    for i in (0, 1, 3, 4, 5, 6):                 # row_map alone may be missing
+        assert lib.bm_grouped_matmul(d, *but(7, i, None), None) == NULL, i
+    for i in (0, 4, 6):
+        assert lib.bm_grouped_matmul(d, *but(7, i, ODD), None) == ALIGN, i
+    for i in (0, 1, 3, 4, 5, 6, 7, 8, 9):
+        assert lib.bm_grouped_swiglu(d, *but(10, i, None), None) == NULL, i
+    for i in (0, 4, 6, 8):
+        assert lib.bm_grouped_swiglu(d, *but(10, i, ODD), None) == ALIGN, i
+    # without a map every output row needs its own row of a; without offsets there is one group
+    assert lib.bm_grouped_matmul(ctypes.byref(_product(a_rows=7)), ONE, ONE, None, ONE, ONE, ONE, ONE, None) == SHAPE
+    assert lib.bm_grouped_matmul(ctypes.byref(_product(E=2)), ONE, ONE, None, None, ONE, ONE, ONE, None) == NULL
+
+
+def _layer(**over):
+    return bm.LayerDesc(**dict(dict(T=16, d=64, E=8, F=128, K=2, n_shared=0, R=3, H=3, dtype=bm.BM_BF16, flags=bm.BM_RENORM_TOPK), **over))
+
+
+def test_layer_workspace_bytes():
+    small, big = bm.bm_workspace_bytes_quantized(_layer()), bm.bm_workspace_bytes_quantized(_layer(T=4096))
+    assert 0 < small < big and small % 256 == 0
+    last = 0
+    for T in (0, 1, 16, 255, 256, 257, 300, 512, 513, 4096):             # from fp32 to bf16 expert outputs it must not shrink
+        now = bm.bm_workspace_bytes_quantized(_layer(T=T))
+        assert now >= last, T
+        last = now
+    for over in (dict(dtype=bm.BM_F32), dict(K=9), dict(d=48), dict(F=48), dict(F=32800), dict(n_shared=9), dict(T=-1), dict(E=257)):
+        assert bm.bm_workspace_bytes_quantized(_layer(**over)) == 0, over
+    assert bm.load_library().bm_workspace_bytes_quantized(None) == 0
+
+
+def test_layer_refusals():
+    lib = bm.load_library()
+    n = len(bm.QuantizedWeights._fields_)
+    names = [f[0] for f in bm.QuantizedWeights._fields_]
+
+    def call(d=None, x=ONE, xq=ONE, xs=ONE, w=None, bitmap=ONE, table=ONE, y=ONE, ws=ONE, nbytes=1 << 40):
+        w = bm.QuantizedWeights(*([256] * n)) if w is None else w
+        return lib.bm_moe_forward_quantized(ctypes.byref(d or _layer()), x, xq, xs, ctypes.byref(w), bitmap, table, y, ws, nbytes, None, None)
+
+    assert lib.bm_moe_forward_quantized(None, ONE, ONE, ONE, None, ONE, ONE, ONE, ONE, 1 << 40, None, None) == NULL
+    assert call(_layer(dtype=bm.BM_F32)) == DTYPE
+    assert call(_layer(H=4)) == SHAPE and call(_layer(d=48)) == SHAPE and call(_layer(F=32800)) == SHAPE
+    for kw in (dict(x=None), dict(y=None), dict(bitmap=None), dict(table=None), dict(xq=None), dict(xs=None)):
+        assert call(**kw) == NULL, kw
+    for i, name in enumerate(names):
+        w = bm.QuantizedWeights(*[0 if j == i else 256 for j in range(n)])
+        if not name.startswith("ws_") and name not in ("router_bias", "buddy_q"):
+            assert call(w=w) == NULL, name
+        if name.startswith("ws_"):
+            assert call(_layer(n_shared=1), w=w) == NULL, name
+        if name == "buddy_q":
+            assert call(_layer(flags=bm.BM_PSI_TOKEN), w=w) == NULL
+        if name in ("w_gate", "w_up", "w_down", "ws_gate", "ws_up", "ws_down"):
+            assert call(w=bm.QuantizedWeights(*[264 if j == i else 256 for j in range(n)])) == ALIGN, name
+    assert call(xq=ODD) == ALIGN and call(x=ODD) == ALIGN
+    assert call(ws=None) == WORKSPACE and call(ws=ODD) == WORKSPACE
+    need = bm.bm_workspace_bytes_quantized(_layer())
+    assert call(nbytes=need - 1) == WORKSPACE
+    assert call(_layer(T=0), x=None, y=None, ws=None, nbytes=0) == 0

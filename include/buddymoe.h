@@ -361,8 +361,8 @@ typedef struct {
  * E = 1: one group of all rows.  Products of a block of 128 are summed by the matrix
  * unit in fp32, blocks are scaled and added in fp32 in order; c is rounded once.  Rows of
  * c behind offsets[E] are left as they were, groups without rows read nothing.  Offsets
- * are taken as clamped to [0, rows], mapped rows as clamped to [0, a_rows).
- * Equal calls give equal bits. */
+ * are taken as clamped to [0, rows] and no smaller than those before them, mapped
+ * rows as clamped to [0, a_rows).  Equal calls give equal bits. */
 int bm_grouped_matmul(const bm_product_desc *desc, const void *a, const float *a_scale, const int32_t *row_map,
                       const int32_t *offsets, const void *w, const float *w_scale, void *c, void *stream);
 

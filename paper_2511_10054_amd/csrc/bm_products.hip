@@ -1,9 +1,14 @@
 // Grouped products of 8-bit rows with 8-bit matrices, a 32-bit scale for each 128 values of a row and for each 128 x 128
 // block of a matrix:
 //   c[i][n] = sum_kb sa[i][kb] * sw[n / 128][kb] * sum_{k in block kb} a[i][k] * w[n][k]
-// The inner sum is one v_mfma_f32_16x16x128 (its 128 products are exact, its sum is held in 32 bits); the outer one is a
-// fused multiply-add per value in 32 bits.  Weights are the matrix instruction's row operand and tokens its column
-// operand, so that a lane's four results belong to one token and a block of weights: one scale for all four.
+// The inner sum is made by matrix instructions, the outer one by a fused multiply-add per value in 32 bits.  Weights are the
+// matrix instruction's row operand and tokens its column operand, so that a lane's four results belong to one token and
+// a block of weights: one scale for all four.
+//
+// Two forms of the inner sum.  v_mfma_f32_16x16x128 multiplies e4m3 as it is, 8192 flop a cycle and unit, but cuts each of the
+// eight products that it adds at once below 2^-13 of the largest of them (measured: 1.4e-5 of the result's 2-norm, whatever
+// the instruction's shape): it serves results that are rounded to bf16.  Results in 32 bits - sums that stay so, and h, whose
+// scales are 32-bit numbers - widen e4m3 to fp16, which is exact, for v_mfma_f32_16x16x32_f16 at half the rate (7e-8).
 #include "bm_products.h"
 
 namespace bm {
@@ -44,6 +49,19 @@ __device__ __forceinline__ f32x4 block_product(const Operand<true> &a, const Ope
     for (int i = 0; i < 4; ++i) r = __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v[i], b.v[i], r, 0, 0, 0);
     return r;
 }
+// Two blocks of weights with the same tokens, their chains of matrix instructions interleaved
+__device__ __forceinline__ void block_products(const Operand<false> &a0, const Operand<false> &a1, const Operand<false> &b, f32x4 &r0, f32x4 &r1) {
+    r0 = block_product(a0, b);
+    r1 = block_product(a1, b);
+}
+__device__ __forceinline__ void block_products(const Operand<true> &a0, const Operand<true> &a1, const Operand<true> &b, f32x4 &r0, f32x4 &r1) {
+    r0 = r1 = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(a0.v[i], b.v[i], r0, 0, 0, 0);
+        r1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(a1.v[i], b.v[i], r1, 0, 0, 0);
+    }
+}
 
 #define BM_LDS __attribute__((address_space(3)))
 // At most n direct loads of this wave are still in flight and its LDS accesses are done; then all waves meet.
@@ -53,312 +71,616 @@ __device__ __forceinline__ f32x4 block_product(const Operand<true> &a, const Ope
         __builtin_amdgcn_s_waitcnt(((n) & 15) | (7 << 4) | (((n) >> 4) << 14));         \
         asm volatile("s_barrier" ::: "memory");                                         \
     }
+// The same for a wave whose LDS is its own
+#define BM_WAIT_OWN(n)                                                                  \
+    {                                                                                   \
+        __builtin_amdgcn_s_waitcnt(((n) & 15) | (7 << 4) | (((n) >> 4) << 14));         \
+        asm volatile("" ::: "memory");                                                  \
+    }
 
-// One workgroup's tile: rows [row0, row0 + BM) of a group that ends at row_end, columns [n0, ..).
+// The tile of a workgroup: rows [row0, ..) of a group that ends at row_end, column tile nt.
 struct Tile {
     int group, row0, row_end, nt;
 };
 
-// Which tile a workgroup has.  Tiles are numbered group by group, inside a group by column tile and then by row tile
-// (neighbours share their weights), and each XCD takes a contiguous share: workgroups go round-robin to the XCDs.  Every
-// wave derives the groups' tile counts itself from the offsets (clamped: whatever they hold, no tile leaves the rows).
-template <int BM>
-__device__ __forceinline__ bool find_tile(const ProductParams &p, int n_nt, Tile &t) {
+// The groups' row ranges and tile counts, in LDS.  Offsets are clamped to the rows and raised to the largest before them: whatever
+// they hold, groups do not overlap and no tile leaves the rows.
+struct TileTable {
+    int first[BM_MAX_E + 8 + 1];        // tiles of height bm before the group; [n_groups]: all
+    int lo[BM_MAX_E + 8 + 1];           // first row; the group ends where the next begins
+};
+
+// Called by one wave; the workgroup has to meet before the table is read.
+__device__ __forceinline__ void build_tile_table(const ProductParams &p, int bm, TileTable &tt) {
     const int lane = lane_id();
-    constexpr int CH = (BM_MAX_E + 8 + WAVE - 1) / WAVE;
-    int lo[CH], hi[CH], first[CH], total = 0;
+    int total = 0, last = p.offsets ? min(max(ldg_i32(p.offsets), 0), p.rows) : 0;
+    for (int c = 0; c < p.n_groups; c += WAVE) {
+        const int g = c + lane;
+        int hi = last;
+        if (g < p.n_groups) hi = p.offsets ? min(max(ldg_i32(p.offsets + g + 1), last), p.rows) : p.rows;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int g = c * WAVE + lane;
-        lo[c] = hi[c] = 0;
+        for (int s = 1; s < WAVE; s <<= 1) {
+            const int o = __shfl_up(hi, s, WAVE);
+            hi = lane >= s ? max(hi, o) : hi;
+        }
+        const int before = __shfl_up(hi, 1, WAVE), lo = lane ? before : last;
+        const int mine = (hi - lo + bm - 1) / bm;
+        int sum = mine;
+#pragma unroll
+        for (int s = 1; s < WAVE; s <<= 1) {
+            const int o = __shfl_up(sum, s, WAVE);
+            sum += lane >= s ? o : 0;
+        }
         if (g < p.n_groups) {
-            lo[c] = p.offsets ? min(max(ldg_i32(p.offsets + g), 0), p.rows) : 0;
-            hi[c] = p.offsets ? min(max(ldg_i32(p.offsets + g + 1), lo[c]), p.rows) : p.rows;
+            tt.first[g] = total + sum - mine;
+            tt.lo[g] = lo;
         }
+        total += __builtin_amdgcn_readlane(sum, WAVE - 1);
+        last = __builtin_amdgcn_readlane(hi, WAVE - 1);
     }
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        first[c] = total;
-        if (c * WAVE < p.n_groups) {
-            const int mine = (hi[c] - lo[c] + BM - 1) / BM;
-            int sum = mine;
-#pragma unroll
-            for (int s = 1; s < WAVE; s <<= 1) {
-                const int o = __shfl_up(sum, s, WAVE);
-                sum += lane >= s ? o : 0;
-            }
-            first[c] = total + sum - mine;
-            total += __builtin_amdgcn_readlane(sum, WAVE - 1);
-        }
+    if (lane == 0) {
+        tt.first[p.n_groups] = total;
+        tt.lo[p.n_groups] = last;
     }
-    const long long tiles = (long long)total * n_nt, per_xcd = (tiles + 7) >> 3;
-    const long long lid = (long long)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-    if ((long long)(blockIdx.x >> 3) >= per_xcd || lid >= tiles) return false;
-    const int m = (int)(lid / n_nt);           // the row tiles before it belong to whole groups before it
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int n = (hi[c] - lo[c] + BM - 1) / BM;
-        const unsigned long long hit = __ballot(n > 0 && first[c] <= m && m < first[c] + n);
-        if (hit) {
-            const int src = __ffsll((unsigned long long)hit) - 1;
-            const int f = __builtin_amdgcn_readlane(first[c], src), nn = __builtin_amdgcn_readlane(n, src);
-            const int in = (int)(lid - (long long)f * n_nt);
-            t.group = c * WAVE + src;
-            t.nt = in / nn;
-            t.row0 = __builtin_amdgcn_readlane(lo[c], src) + (in % nn) * BM;
-            t.row_end = __builtin_amdgcn_readlane(hi[c], src);
-            return true;
-        }
-    }
-    return false;
 }
+
+// Tiles are numbered group by group, inside a group by column tile and then by row tile (neighbours share their weights).
+__device__ __forceinline__ Tile tile_at(const ProductParams &p, const TileTable &tt, int bm, int n_nt, int lid) {
+    const int lane = lane_id(), m = lid / n_nt;        // the row tiles before it belong to whole groups before it
+    Tile t{};
+    for (int c = 0; c < p.n_groups; c += WAVE) {
+        const int g = min(c + lane, p.n_groups - 1);
+        const int f = tt.first[g], n = tt.first[g + 1] - f;
+        const unsigned long long hit = __ballot(c + lane < p.n_groups && f <= m && m < f + n);
+        if (hit) {
+            const int src = __ffsll(hit) - 1, f0 = __builtin_amdgcn_readlane(f, src), rows_n = __builtin_amdgcn_readlane(n, src);
+            const int in = lid - f0 * n_nt;
+            t.group = c + src;
+            t.nt = in / rows_n;
+            t.row0 = __builtin_amdgcn_readfirstlane(tt.lo[t.group]) + (in % rows_n) * bm;
+            t.row_end = __builtin_amdgcn_readfirstlane(tt.lo[t.group + 1]);
+            break;
+        }
+    }
+    return t;
+}
+
+// Every XCD takes a contiguous share of the tiles; workgroups go round-robin to the XCDs, so blockIdx.x % 8 names it.
+struct Share {
+    int begin, end, step;
+};
+__device__ __forceinline__ Share my_share(int tiles) {
+    const int per_xcd = (tiles + 7) >> 3, from = min((int)(blockIdx.x & 7) * per_xcd, tiles);
+    return Share{from + (int)(blockIdx.x >> 3), min(from + per_xcd, tiles), (int)(gridDim.x >> 3)};
+}
+
+// Row of a for output row `row` of a group that ends at row_end (past the end: the last one's)
+__device__ __forceinline__ int row_of_id(const ProductParams &p, int id) { return min(max(id / p.map_div, 0), p.a_rows - 1); }
+__device__ __forceinline__ int source_row(const ProductParams &p, int row, int row_end) {
+    const int pos = min(row, row_end - 1);
+    return p.row_map ? row_of_id(p, ldg_i32(p.row_map + pos)) : min(pos, p.a_rows - 1);
+}
+
+// A lane's 32 values of row pos of a stage: pieces q4 and q4 + 4 (any order serves, the same for both operands)
+__device__ __forceinline__ i32x8 lds_operand(const uint8_t *rows, int pos, int q4) {
+    const int x = (pos >> 1) & 7;
+    const u32x4 lo = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + ((q4 ^ x) * 16));
+    const u32x4 hi = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + (((q4 + 4) ^ x) * 16));
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+}
+
+// The block of 128 at which a streaming tile's walk along the reduction begins (it goes round).  Workgroups that start together
+// would otherwise read the same offset of their rows at the same time, which lie a power of two apart in many layers, and
+// meet in few memory channels (5 % of the gate/up product of one token).  A function of the group and the columns: a row's sum does
+// not depend on the rest of the batch.
+__device__ __forceinline__ int entry_block(const Tile &t, int kb_n) { return (t.group * 7 + t.nt * 5) % kb_n; }
+
+// Four consecutive values of c
+__device__ __forceinline__ void store4(const ProductParams &p, size_t at, f32x4 v) {
+    if (p.c_f32) *(BM_GLOBAL f32x4 *)(static_cast<float *>(p.c) + at) = v;
+    else *(BM_GLOBAL u32x2 *)(static_cast<uint16_t *>(p.c) + at) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
+// The group's matrices and their scales
+struct Matrices {
+    const uint8_t *w0, *w1;
+    const float *s0, *s1;
+};
+template <bool DUAL>
+__device__ __forceinline__ Matrices matrices_of(const ProductParams &p, int group) {
+    const int kb_n = (p.Kd + SCALE_BLOCK - 1) / SCALE_BLOCK, nb_n = (p.N + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    const bool routed = group < p.E;
+    const size_t g = routed ? group : group - p.E, at = g * p.N * p.Kd, sat = g * nb_n * kb_n;
+    return Matrices{(routed ? p.b0 : p.sb0) + at, DUAL ? (routed ? p.b1 : p.sb1) + at : nullptr,
+                    (routed ? p.bs0 : p.sbs0) + sat, DUAL ? (routed ? p.bs1 : p.sbs1) + sat : nullptr};
+}
+
+__device__ uint4 zero_piece;             // where pieces of tokens past the row's end come from
 
 }  // namespace
 
-// BM tokens x BN weight rows (DUAL: BN / 2 of the gate, BN / 2 of the up matrix) per workgroup of NW waves, WNN of them along
-// the weight rows.  Steps of 128 along the reduction go through a ring of S stages in LDS, filled with direct loads (a row's
-// 128 bytes are one cache line; 8 rows an instruction).  Piece p of row r lies in slot p ^ ((r >> 1) & 7), so that the 16
-// rows of an operand read fall into different banks.
-template <int BM, int BN, int NW, int WNN, int S, bool DUAL, bool WIDE>
-__global__ void __launch_bounds__(NW * 64) product_kernel(ProductParams p) {
-    constexpr int WMN = NW / WNN;
+// ---------------------------------------------------------------------------------------------------------------------
+// Tiles of BM tokens x 256 weight rows (DUAL: 128 of the gate, 128 of the up matrix) on 8 waves, WNN of them along the weight
+// rows.  The reduction goes in steps of 128 through two rings in LDS, SW stages of weights and ST of tokens, filled with
+// direct loads: a row's 128 bytes are one cache line, 8 rows an instruction.  Piece p of row r lies in slot p ^ ((r >> 1) & 7),
+// so that the 16 rows of an operand read fall into different banks.
+//
+// A workgroup takes one tile after the other and its loads run ahead across them: the last steps of a tile fetch the first
+// blocks of the next, whose rows and scales were fetched at the tile's beginning.  A step waits for the loads that it needs
+// and leaves those behind them in flight (AHEAD; loads return in order, and whatever else is in flight only makes the
+// wait stricter).
+//   step s:  tokens of step s and weights of step s have landed -> all waves meet (so the stages read in step s - 1 are
+//   free) -> load the tokens of step s + ST - 1 and the weights of step s + SW - 1 -> multiply.
+// NEAR: the reduction is a multiple of 128, at least MIN_STEPS blocks, and a is smaller than 4 GiB: no piece is cut, addresses are
+// 32-bit offsets (which leaves room for tiles of 192 tokens).
+// Everything lies in one LDS array: of several, the compiler tells apart which one direct loads fill, and holds every read
+// of that one until no load is in flight.
+// ---------------------------------------------------------------------------------------------------------------------
+template <int BM, int WNN, int SW, int ST, int PER_UNIT, bool DUAL, bool WIDE, bool NEAR>
+__global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams p) {
+    constexpr int NW = 8, BN = 256, WMN = NW / WNN;
     constexpr int TB = BM / WMN / 16, WB = BN / WNN / 16;      // 16-token and 16-row blocks of a wave
     constexpr int HB = DUAL ? WB / 2 : WB;                     // of these, blocks of different columns
     constexpr int COLS = DUAL ? BN / 2 : BN;
     constexpr int WI = BN / NW / 8;                            // weight loads of a wave and stage
     constexpr int TR = BM / NW, TI = TR >= 8 ? TR / 8 : 1;     // token rows and loads of a wave and stage
     constexpr int PER = WI + TI + 1;                           // with the tokens' scales
-    constexpr int STAGE = (BN + BM) * 128;
-    static_assert(WI * 8 * NW == BN && TB * 16 * WMN == BM && WB * 16 * WNN == BN && (TR >= 8 ? TR % 8 == 0 : TR > 0), "tile shape");
-    static_assert(!DUAL || COLS == SCALE_BLOCK, "a tile quantizes whole blocks");
-    static_assert((S - 2) * PER < 64, "the wait counts up to 63 loads");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[S * STAGE];
-    __shared__ float s_sa[S * BM];
-    __shared__ float s_sw[DUAL ? 2 : (BN + SCALE_BLOCK - 1) / SCALE_BLOCK + 1][MAX_PRODUCT_KD / SCALE_BLOCK];
-    __shared__ float s_amax[DUAL ? WNN : 1][DUAL ? BM : 1];
+    constexpr int AHEAD = ST < SW ? WI + (ST - 2) * PER : (ST - 2) * PER;
+    constexpr int PART = BM <= 64 ? 1 : TB;                    // blocks that are multiplied or, where no token is theirs, left out together
+    constexpr int MIN_STEPS = 4;                               // shorter walks are filled up with blocks of zeros
+    static_assert(TB * 16 * WMN == BM && WB * 16 * WNN == BN && (TR >= 8 ? TR % 8 == 0 : TR > 0), "tile shape");
+    static_assert(ST <= SW && SW <= MIN_STEPS && AHEAD < 64, "stages");
+    constexpr int MAX_KB = MAX_PRODUCT_KD / SCALE_BLOCK;
+    constexpr int W_BYTES = SW * BN * 128, T_BYTES = ST * BM * 128;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[W_BYTES + T_BYTES + (ST * BM + 4 * MAX_KB + BM + (DUAL ? WNN * BM : 0)) * 4 + sizeof(TileTable)];
+    uint8_t *const w_ring = lds, *const t_ring = lds + W_BYTES;
+    float *const s_sa = reinterpret_cast<float *>(t_ring + T_BYTES);              // [ST][BM] tokens' scales
+    float *const s_sw = s_sa + ST * BM;                                           // [2 tiles][2][MAX_KB] weight blocks' scales
+    int *const s_id = reinterpret_cast<int *>(s_sw + 4 * MAX_KB);                 // [BM] row_map of the next tile
+    uint32_t *const s_amax = reinterpret_cast<uint32_t *>(s_id + BM);             // [WNN][BM]
+    TileTable &tt = *reinterpret_cast<TileTable *>(s_amax + (DUAL ? WNN * BM : 0));
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int wm = wave / WNN, wn = wave % WNN;
-    const int q4 = lane >> 4, l16 = lane & 15;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wm = wave / WNN, wn = wave % WNN, q4 = lane >> 4, l16 = lane & 15;
     const int N = p.N, Kd = p.Kd, kb_n = (Kd + SCALE_BLOCK - 1) / SCALE_BLOCK, nb_n = (N + SCALE_BLOCK - 1) / SCALE_BLOCK;
-    Tile t;
-    if (!find_tile<BM>(p, (N + COLS - 1) / COLS, t)) return;
-    const int g = __builtin_amdgcn_readfirstlane(t.group), row0 = t.row0, row_end = t.row_end;
-    const int n0 = t.nt * COLS;
-    const bool routed = g < p.E;
-    const size_t ge = routed ? g : g - p.E;
-    const uint8_t *b0 = (routed ? p.b0 : p.sb0) + ge * N * Kd, *b1 = DUAL ? (routed ? p.b1 : p.sb1) + ge * N * Kd : nullptr;
-    const float *bs0 = (routed ? p.bs0 : p.sbs0) + ge * nb_n * kb_n, *bs1 = DUAL ? (routed ? p.bs1 : p.sbs1) + ge * nb_n * kb_n : nullptr;
+    const int n_nt = (N + COLS - 1) / COLS, KT = NEAR ? kb_n : max(kb_n, MIN_STEPS);
 
-    // weight scales of the tile's blocks
-    {
-        constexpr int NBT = DUAL ? 2 : (BN + SCALE_BLOCK - 1) / SCALE_BLOCK + 1;
-        for (int i = tid; i < NBT * kb_n; i += NW * 64) {
-            const int j = i / kb_n, kb = i - j * kb_n;
-            s_sw[j][kb] = DUAL ? ldg_f32((j ? bs1 : bs0) + (size_t)(n0 / SCALE_BLOCK) * kb_n + kb)
-                               : ldg_f32(bs0 + (size_t)min(n0 / SCALE_BLOCK + j, nb_n - 1) * kb_n + kb);
-        }
-    }
+    if (wave == 0) build_tile_table(p, BM, tt);
+    BM_WAIT_AND_MEET(0)
+    const Share share = my_share(__builtin_amdgcn_readfirstlane(tt.first[p.n_groups]) * n_nt);
+    if (share.begin >= share.end) return;
 
-    // addresses of this wave's loads: whole rows of 128 bytes, 8 an instruction
-    const uint8_t *wp[WI], *tp[TI];
-    int wpc[WI], tpc[TI];
-#pragma unroll
-    for (int j = 0; j < WI; ++j) {
-        const int pos = wave * (WI * 8) + j * 8 + (lane >> 3);        // row in the stage
-        const int b = (pos >> 4) % WB, m = pos & 15, w = (pos >> 4) / WB;
-        const int bb = DUAL ? b % HB : b;
-        // a lane's results of all blocks are consecutive columns
-        const int n = min(n0 + w * (16 * HB) + (m >> 2) * (4 * HB) + bb * 4 + (m & 3), N - 1);
-        wpc[j] = (lane & 7) ^ ((pos >> 1) & 7);
-        wp[j] = (DUAL && b >= HB ? b1 : b0) + (size_t)n * Kd + wpc[j] * 16;
-    }
-    auto source_row = [&](int r) {                                     // row of a for row r of the tile (past the end: the last one)
-        const int pos = min(row0 + r, row_end - 1);
-        const int src = p.row_map ? ldg_i32(p.row_map + pos) / p.map_div : pos;
-        return min(max(src, 0), p.a_rows - 1);
-    };
-    const bool tl = TR >= 8 || lane < TR * 8;                          // lanes with a token piece
-#pragma unroll
-    for (int j = 0; j < TI; ++j) {
-        const int pos = wave * TR + j * 8 + (TR >= 8 ? lane >> 3 : min(lane >> 3, TR - 1));
-        tpc[j] = (lane & 7) ^ ((pos >> 1) & 7);
-        tp[j] = p.a + (size_t)source_row(pos) * Kd + tpc[j] * 16;
-    }
-    const bool sl = lane < TR;                                         // lanes with a token's scale
-    const float *sp = p.a_scale + (size_t)source_row(wave * TR + min(lane, TR - 1)) * kb_n;
-
-    auto issue = [&](int kt) {
-        const int st = kt % S;
-        uint8_t *base = smem + st * STAGE;
-        const int k0 = kt * 128;
-        const bool cut = k0 + 128 > Kd;                                // pieces past the row's end: a piece of the row instead
+    // ---- loading side: the tile whose weights are fetched, the tile whose tokens are fetched ----
+    Matrices wt;                                               // at the tile's first row
+    uint32_t wo[WI];                                           // 32 bits: 256 rows of at most 32768 bytes
+    int w_entry = 0;
+    const uint8_t *tp[NEAR ? 1 : TI];
+    const float *sp = nullptr;
+    uint32_t to[NEAR ? TI : 1], so = 0;
+    int t_entry = 0;
+    auto w_piece = [&](int j) { return (lane & 7) ^ (((wave * (WI * 8) + j * 8 + (lane >> 3)) >> 1) & 7); };
+    auto t_pos = [&](int j) { return wave * TR + j * 8 + (TR >= 8 ? lane >> 3 : min(lane >> 3, TR - 1)); };
+    auto t_piece = [&](int j) { return (lane & 7) ^ ((t_pos(j) >> 1) & 7); };
+    auto entry_of = [&](const Tile &t) { return BM <= 64 && kb_n >= MIN_STEPS ? entry_block(t, kb_n) : 0; };
+    auto aim_weights = [&](const Tile &t) {
+        const int n0 = t.nt * COLS;
+        wt = matrices_of<DUAL>(p, t.group);
+        wt.w0 += (size_t)n0 * Kd;
+        if (DUAL) wt.w1 += (size_t)n0 * Kd;
+        w_entry = entry_of(t);
 #pragma unroll
         for (int j = 0; j < WI; ++j) {
-            const uint8_t *src = wp[j] + k0;
-            if (cut && k0 + wpc[j] * 16 >= Kd) src -= wpc[j] * 16;
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)(base + (wave * (WI * 8) + j * 8) * 128), 16, 0, 0);
+            const int pos = wave * (WI * 8) + j * 8 + (lane >> 3);                // row in the stage
+            const int b = (pos >> 4) % WB, m = pos & 15, w = (pos >> 4) / WB, bb = DUAL ? b % HB : b;
+            // a lane's results of all blocks are consecutive columns
+            const int n = min(w * (16 * HB) + (m >> 2) * (4 * HB) + bb * 4 + (m & 3), N - 1 - n0);
+            wo[j] = (uint32_t)n * (uint32_t)Kd + w_piece(j) * 16;
         }
+    };
+    // rows by their ids in LDS (row r of the tile at s_id[r]), or by row_map
+    auto aim_tokens = [&](const Tile &t, bool ids) {
+        auto row = [&](int pos) {
+            if (!ids || !p.row_map) return source_row(p, t.row0 + pos, t.row_end);
+            return row_of_id(p, s_id[pos]);
+        };
 #pragma unroll
         for (int j = 0; j < TI; ++j) {
-            const uint8_t *src = tp[j] + k0;
-            if (cut && k0 + tpc[j] * 16 >= Kd) src -= tpc[j] * 16;
-            if (tl) __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)(base + (BN + wave * TR + j * 8) * 128), 16, 0, 0);
+            if constexpr (NEAR) to[j] = (uint32_t)row(t_pos(j)) * (uint32_t)Kd + t_piece(j) * 16;
+            else tp[j] = p.a + (size_t)row(t_pos(j)) * Kd + t_piece(j) * 16;
         }
-        if (sl) __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(sp + kt), (BM_LDS void *)(s_sa + st * BM + wave * TR), 4, 0, 0);
+        if constexpr (NEAR) so = (uint32_t)row(wave * TR + min(lane, TR - 1)) * (uint32_t)kb_n;
+        else sp = p.a_scale + (size_t)row(wave * TR + min(lane, TR - 1)) * kb_n;
+        t_entry = entry_of(t);
+    };
+    auto block_at = [&](int step, int entry) { return step + entry < KT ? step + entry : step + entry - KT; };
+    // Pieces past the row's end: of weights any piece of the row, of tokens zeros.  Blocks past the last one: the first, and zeros.
+    auto load_weights = [&](int step, int slot) {
+        const int kt = block_at(step, w_entry), k0 = NEAR || kt < kb_n ? kt * 128 : 0;
+        uint8_t *base = w_ring + slot * (BN * 128);
+#pragma unroll
+        for (int j = 0; j < WI; ++j) {
+            const int pos = wave * (WI * 8) + j * 8, pc = w_piece(j) * 16;
+            const uint8_t *from = (DUAL && (pos >> 4) % WB >= HB ? wt.w1 : wt.w0) + k0;
+            const uint32_t off = NEAR || k0 + pc < Kd ? wo[j] : wo[j] - pc;
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(from + off), (BM_LDS void *)(base + pos * 128), 16, 0, 0);
+        }
+    };
+    auto load_tokens = [&](int step, int slot) {
+        const int kt = block_at(step, t_entry), k0 = kt * 128;
+        uint8_t *base = t_ring + slot * (BM * 128);
+#pragma unroll
+        for (int j = 0; j < TI; ++j) {
+            const uint8_t *src;
+            if constexpr (NEAR) src = p.a + k0 + to[j];
+            else src = k0 + t_piece(j) * 16 < Kd ? tp[j] + k0 : reinterpret_cast<const uint8_t *>(&zero_piece);
+            if (TR >= 8 || lane < TR * 8)
+                __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)(base + (wave * TR + j * 8) * 128), 16, 0, 0);
+        }
+        const float *sc;
+        if constexpr (NEAR) sc = p.a_scale + kt + so;
+        else sc = sp + min(kt, kb_n - 1);
+        if (lane < TR)
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)sc, (BM_LDS void *)(s_sa + slot * BM + wave * TR), 4, 0, 0);
+    };
+    // What a tile needs beside its operands: the scales of its weight blocks (a wave fetches 64 of one of two rows) and its rows' ids
+    auto load_meta = [&](const Tile &t, int buf, bool ids) {
+        const int j = wave >> 2, kb = (wave & 3) * 64 + lane, nb = min(t.nt * COLS / SCALE_BLOCK + (DUAL ? 0 : j), nb_n - 1);
+        const Matrices m = matrices_of<DUAL>(p, t.group);
+        const float *s = (DUAL && j ? m.s1 : m.s0) + (size_t)nb * kb_n;
+        if (kb < kb_n)
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(s + kb), (BM_LDS void *)(s_sw + (buf * 2 + j) * MAX_KB + (wave & 3) * 64), 4, 0, 0);
+        if (ids && p.row_map && lane < TR)
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(p.row_map + min(t.row0 + wave * TR + lane, t.row_end - 1)),
+                                             (BM_LDS void *)(s_id + wave * TR), 4, 0, 0);
     };
 
+    int lid = share.begin;
+    Tile cur = tile_at(p, tt, BM, n_nt, lid), next{};
+    aim_weights(cur);
+    aim_tokens(cur, false);
+    load_meta(cur, 0, false);
+    int w_slot = 0, t_slot = 0;                                // next stages to fill
+    auto advance = [](int &slot, int n) { slot = slot + 1 == n ? 0 : slot + 1; };
+#pragma unroll
+    for (int s = 1 - SW; s < 0; ++s) {
+        if (s + ST - 1 >= 0) { load_tokens(s + ST - 1, t_slot); advance(t_slot, ST); }
+        load_weights(s + SW - 1, w_slot);
+        advance(w_slot, SW);
+    }
+    int w_read = 0, t_read = 0, buf = 0;                       // stages and scales that are read
+
+    while (true) {
+        const bool more = lid + share.step < share.end;
+        const int live = min(cur.row_end - cur.row0, BM) - wm * (TB * 16), entry = entry_of(cur);
+        f32x4 acc[WB][TB];
+#pragma unroll
+        for (int b = 0; b < WB; ++b)
+#pragma unroll
+            for (int i = 0; i < TB; ++i) acc[b][i] = 0.0f;
+
+        for (int step = 0; step < KT; ++step) {
+            if (more || step + SW - 2 < KT) BM_WAIT_AND_MEET(AHEAD)
+            else BM_WAIT_AND_MEET(0)
+            if (step == 0 && more) {
+                next = tile_at(p, tt, BM, n_nt, lid + share.step);
+                load_meta(next, buf ^ 1, true);
+            }
+            if (step + ST - 1 < KT || more) {
+                if (step + ST - 1 == KT) aim_tokens(next, true);
+                load_tokens(step + ST - 1 < KT ? step + ST - 1 : step + ST - 1 - KT, t_slot);
+                advance(t_slot, ST);
+            }
+            if (step + SW - 1 < KT || more) {
+                if (step + SW - 1 == KT) aim_weights(next);
+                load_weights(step + SW - 1 < KT ? step + SW - 1 : step + SW - 1 - KT, w_slot);
+                advance(w_slot, SW);
+            }
+            const uint8_t *ws = w_ring + w_read * (BN * 128), *ts = t_ring + t_read * (BM * 128);
+            const float *sa_at = s_sa + t_read * BM + wm * (TB * 16) + l16;
+            const int kt = NEAR ? block_at(step, entry) : min(block_at(step, entry), kb_n - 1);
+            // DUAL: the gate's and the up matrix's scale; else one of the two blocks of 128 columns, the wave's
+            const float sw0 = s_sw[(buf * 2 + (DUAL ? 0 : wn * (16 * HB) / SCALE_BLOCK)) * MAX_KB + kt];
+            const float sw1 = DUAL ? s_sw[(buf * 2 + 1) * MAX_KB + kt] : sw0;
+            if (BM > 64 && live <= 0) { advance(w_read, SW); advance(t_read, ST); continue; }
+            Operand<WIDE> wf[WB];
+#pragma unroll
+                for (int b = 0; b < WB; ++b) wf[b].set(lds_operand(ws, (wn * WB + b) * 16 + l16, q4));
+#pragma unroll
+            for (int i0 = 0; i0 < TB; i0 += PART) {
+                if (BM <= 64 && live <= i0 * 16) break;              // (in large tiles the branch costs 60 spilled registers)
+                // operands of the next 16 tokens are read, and the results of the block before are added, under the matrix
+                // instructions of the present one
+                const int pos0 = wm * (TB * 16) + i0 * 16 + l16;
+                i32x8 raw = lds_operand(ts, pos0, q4);
+                float sa[PART];
+#pragma unroll
+                for (int i = 0; i < PART; ++i) sa[i] = sa_at[(i0 + i) * 16];
+                f32x4 r[2][2];
+                Operand<WIDE> tf;
+                auto add = [&](int n) {
+                    const float f = sa[n / WB] * (DUAL && n % WB >= HB ? sw1 : sw0);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[n % WB][i0 + n / WB][v] = fmaf(r[n >> 1 & 1][n & 1][v], f, acc[n % WB][i0 + n / WB][v]);
+                };
+#pragma unroll
+                for (int n = 0; n < PART * WB; n += 2) {
+                    if (n % WB == 0) {
+                        tf.set(raw);
+                        if (n / WB + 1 < PART) raw = lds_operand(ts, pos0 + (n / WB + 1) * 16, q4);
+                    }
+                    block_products(wf[n % WB], wf[n % WB + 1], tf, r[n >> 1 & 1][0], r[n >> 1 & 1][1]);
+                    if (n > 0) {
+                        add(n - 2);
+                        add(n - 1);
+                    }
+                    if (WIDE && BM > 64) __builtin_amdgcn_sched_barrier(0);      // hoisted further, reads and widening cost 4 to 7 %
+                }
+                add(PART * WB - 2);
+                add(PART * WB - 1);
+            }
+            advance(w_read, SW);
+            advance(t_read, ST);
+        }
+
+        // ---- write-out: a lane holds 4 * HB consecutive columns of each of its tokens (N is a multiple of 32: all in or none) ----
+        const int n0 = cur.nt * COLS, col = n0 + wn * (16 * HB) + q4 * (4 * HB), first = wm * (TB * 16) + l16;
+        if constexpr (!DUAL) {
+#pragma unroll
+            for (int i = 0; i < TB; ++i) {
+                const int r = cur.row0 + first + i * 16;
+                if (r >= cur.row_end || col >= N) continue;
+#pragma unroll
+                for (int b = 0; b < WB; ++b) store4(p, (size_t)r * N + col + 4 * b, acc[b][i]);
+            }
+        } else {
+            // h = silu(gate) * up in place of the gate's sums; the largest magnitude of a token's 128 columns over lanes and waves
+            // (as bits: their order is that of non-negative numbers); the scale; the conversion
+            const bool in = col < N;
+#pragma unroll
+            for (int i = 0; i < TB; ++i) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int b = 0; b < HB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float h = in ? silu(acc[b][i][v]) * acc[HB + b][i][v] : 0.0f;
+                        acc[b][i][v] = h;
+                        m = max(m, __builtin_bit_cast(uint32_t, h) & 0x7fffffffu);
+                    }
+                m = max(m, (uint32_t)__shfl_xor((int)m, 16, WAVE));
+                m = max(m, (uint32_t)__shfl_xor((int)m, 32, WAVE));
+                if (q4 == 0) s_amax[wn * BM + first + i * 16] = m;
+            }
+            BM_WAIT_AND_MEET(63)                              // LDS only: loads go on
+#pragma unroll
+            for (int i = 0; i < TB; ++i) {
+                const int at = first + i * 16, r = cur.row0 + at;
+                uint32_t m = 0;
+#pragma unroll
+                for (int w = 0; w < WNN; ++w) m = max(m, s_amax[w * BM + at]);
+                if (r >= cur.row_end) continue;
+                const float s = block_scale(m), inv = 1.0f / s;
+                if (wn == 0 && q4 == 0) p.c_scale[(size_t)r * nb_n + cur.nt] = s;
+                if (!in) continue;
+                uint8_t *c = static_cast<uint8_t *>(p.c) + (size_t)r * N + col;
+#pragma unroll
+                for (int b = 0; b < HB; ++b)
+                    *(BM_GLOBAL uint32_t *)(c + 4 * b) = e4m3x4(quotient(acc[b][i][0], s, inv), quotient(acc[b][i][1], s, inv),
+                                                                quotient(acc[b][i][2], s, inv), quotient(acc[b][i][3], s, inv));
+            }
+        }
+        if (!more) return;
+        cur = next;
+        lid += share.step;
+        buf ^= 1;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// One product of few rows a group: the weights' bytes are what counts.  Every wave streams 32 weight rows through a ring of its
+// own in LDS - whole cache lines, no barrier in the loop - WR waves along the weight rows, WK along the reduction (wave k
+// takes every WK-th block of 128, so that the workgroup reads consecutive lines; the parts are added in order at the end).
+// Tokens go straight to registers, as far ahead as the weights: loads return in order, and waiting for a nearer one would
+// wait for all weights in flight.  Their scales lie in LDS from the start (from memory in the loop they cost as many bytes
+// from the L2 as the tokens: a line for four).
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int STREAM_SCALES = 32 * 112;          // tokens x blocks of 128 whose scales fit beside the ring
+
+template <int TB, int WR, int WK, int S, bool WIDE>
+__device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &t, int rows, uint8_t *ring, const float *s_sw, const float *s_sa,
+                                            const uint8_t *b0) {
+    constexpr int WB = 2, PER = 4 + 2 * TB;
+    static_assert((S - 2) * PER < 64, "the wait counts up to 63 loads");
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wr = wave % WR, wk = wave / WR, q4 = lane >> 4, l16 = lane & 15;
+    const int N = p.N, Kd = p.Kd, kb_n = (Kd + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    const int row0 = t.row0, row_end = t.row_end, n0 = t.nt * (32 * WR);
+    uint8_t *mine = ring + wave * (S * 4096);
+
+    const uint8_t *wp[4];
+    const int piece = (lane & 7) ^ ((lane >> 4) & 3);             // of rows 8 j + lane / 8: (row >> 1) & 7 is 4 (j & 1) more
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int pos = j * 8 + (lane >> 3), b = pos >> 4, m = pos & 15;
+        const int n = min(n0 + wr * 32 + (m >> 2) * 8 + b * 4 + (m & 3), N - 1);         // a lane's results: consecutive columns
+        wp[j] = b0 + (size_t)n * Kd + ((piece ^ (4 * (j & 1))) * 16);
+    }
+    const uint8_t *tp[TB];
+#pragma unroll
+    for (int i = 0; i < TB; ++i) tp[i] = p.a + (size_t)source_row(p, row0 + i * 16 + l16, row_end) * Kd + q4 * 16;
+    u32x4 tlo[S][TB], thi[S][TB];
     f32x4 acc[WB][TB];
 #pragma unroll
     for (int b = 0; b < WB; ++b)
 #pragma unroll
         for (int i = 0; i < TB; ++i) acc[b][i] = 0.0f;
 
-    const int live = min(row_end - row0, BM) - wm * (TB * 16);        // tokens of this wave's blocks
-    const int nb_live = (live + 15) / 16;
-    // the wave's blocks of columns lie in one block of 128
-    const int sw_i = DUAL ? 0 : (n0 % SCALE_BLOCK + wn * (16 * HB)) / SCALE_BLOCK;
-
-    const int KT = kb_n;
+    const int steps = (kb_n - wk + WK - 1) / WK, entry = entry_block(t, kb_n);
+    auto block_of = [&](int step) {
+        const int kt = wk + min(step, steps - 1) * WK + entry;      // past the end: the last one again
+        return kt < kb_n ? kt : kt - kb_n;
+    };
+    auto issue = [&](int step, int st, u32x4 (&lo)[TB], u32x4 (&hi)[TB]) {
+        const int k0 = block_of(step) * 128;
+        // pieces past the row's end: the row's piece 0 of this block instead (arithmetic, no branch around a load)
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s)
-        if (s < KT) issue(s);
-    for (int kt = 0; kt < KT; ++kt) {
-        if (KT - kt > S - 2) BM_WAIT_AND_MEET((S - 2) * PER)
-        else BM_WAIT_AND_MEET(0)
-        if (kt + S - 1 < KT) issue(kt + S - 1);
-        const int st = kt % S;
-        const uint8_t *ws = smem + st * STAGE, *ts = ws + BN * 128;
-        auto frag = [&](const uint8_t *rows, int pos) {
-            const int x = (pos >> 1) & 7;
-            const u32x4 lo = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + ((q4 ^ x) * 16));
-            const u32x4 hi = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + (((q4 + 4) ^ x) * 16));
-            i32x8 f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { f[i] = (int)lo[i]; f[4 + i] = (int)hi[i]; }
-            return f;
-        };
-        Operand<WIDE> wf[WB];
-#pragma unroll
-        for (int b = 0; b < WB; ++b) wf[b].set(frag(ws, (wn * WB + b) * 16 + l16));
-        const float sw0 = s_sw[sw_i][kt], sw1 = DUAL ? s_sw[1][kt] : 0.0f;
-        const int rem = Kd - kt * 128;
+        for (int j = 0; j < 4; ++j) {
+            const int pc = (piece ^ (4 * (j & 1))) * 16, back = k0 + pc >= Kd ? pc : 0;
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(wp[j] + (k0 - back)), (BM_LDS void *)(mine + st * 4096 + j * 1024), 16, 0, 0);
+        }
 #pragma unroll
         for (int i = 0; i < TB; ++i) {
-            if (i < nb_live) {
-                const int pos = wm * (TB * 16) + i * 16 + l16;
-                i32x8 tf = frag(ts, pos);
-                if (rem < 128) {
+            const int at = q4 * 16, lo_at = k0 + at >= Kd ? k0 - at : k0, hi_at = k0 + at + 64 >= Kd ? k0 - at : k0 + 64;
+            lo[i] = ldg128(tp[i] + lo_at);
+            hi[i] = ldg128(tp[i] + hi_at);
+        }
+    };
+    // Loads are issued without a condition (the compiler counts those in flight behind the tokens, and would wait for all of
+    // them where two paths meet); the few past the end come from the L2
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        tf[u] = q4 * 16 < rem ? tf[u] : 0;
-                        tf[4 + u] = q4 * 16 + 64 < rem ? tf[4 + u] : 0;
-                    }
+    for (int s = 0; s < S - 1; ++s) issue(s, s, tlo[s], thi[s]);
+    for (int s0 = 0; s0 < steps; s0 += S) {
+#pragma unroll
+        for (int st = 0; st < S; ++st) {
+            const int step = s0 + st;
+            if (step >= steps) break;
+            BM_WAIT_OWN((S - 2) * PER)
+            constexpr int LAST = S - 1;
+            issue(step + LAST, (st + LAST) % S, tlo[(st + LAST) % S], thi[(st + LAST) % S]);      // the stage read last
+            const int kt = block_of(step);
+            const uint8_t *ws = mine + st * 4096;
+            Operand<WIDE> wf[WB];
+#pragma unroll
+            for (int b = 0; b < WB; ++b) wf[b].set(lds_operand(ws, b * 16 + l16, q4));
+            const float sw = s_sw[kt];
+            const int rem = Kd - kt * 128;
+#pragma unroll
+            for (int i = 0; i < TB; ++i) {
+                u32x4 lo = tlo[st][i], hi = thi[st][i];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {                          // pieces past the row's end count nothing
+                    lo[u] = q4 * 16 < rem ? lo[u] : 0u;
+                    hi[u] = q4 * 16 + 64 < rem ? hi[u] : 0u;
                 }
                 Operand<WIDE> to;
-                to.set(tf);
-                const float sa = s_sa[st * BM + pos];
-                const float f0 = sa * sw0, f1 = sa * sw1;
+                to.set(i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]});
+                const float f = s_sa[min(i * 16 + l16, rows - 1) * kb_n + kt] * sw;
 #pragma unroll
                 for (int b = 0; b < WB; ++b) {
                     const f32x4 r = block_product(wf[b], to);
-                    const float f = DUAL && b >= HB ? f1 : f0;
 #pragma unroll
                     for (int v = 0; v < 4; ++v) acc[b][i][v] = fmaf(r[v], f, acc[b][i][v]);
                 }
             }
         }
     }
-
-    const int col = n0 + wn * (16 * HB) + q4 * (4 * HB);              // this lane's 4 * HB columns
-    if (!DUAL) {
-        if (col >= N) return;                                          // N is a multiple of 32: all of them or none
+    BM_WAIT_OWN(0)                                                     // nothing may land in LDS that others use, or behind the end
+    constexpr int PAIRS = WB * TB;
+    auto put = [&](int b, int i, f32x4 v) {
+        const int col = n0 + wr * 32 + q4 * 8 + b * 4, r = row0 + i * 16 + l16;
+        if (col < N && r < row_end) store4(p, (size_t)r * N + col, v);
+    };
+    if (WK == 1) {
 #pragma unroll
-        for (int i = 0; i < TB; ++i) {
-            const int r = wm * (TB * 16) + i * 16 + l16;
-            if (row0 + r >= row_end) continue;
-            const size_t at = (size_t)(row0 + r) * N + col;
-            if (p.c_f32) {
-#pragma unroll
-                for (int b = 0; b < WB; ++b) *(BM_GLOBAL f32x4 *)(static_cast<float *>(p.c) + at + 4 * b) = acc[b][i];
-            } else {
-#pragma unroll
-                for (int b = 0; b < WB; ++b) {
-                    const u32x2 o = {pack_bf16x2(acc[b][i][0], acc[b][i][1]), pack_bf16x2(acc[b][i][2], acc[b][i][3])};
-                    *(BM_GLOBAL u32x2 *)(static_cast<uint16_t *>(p.c) + at + 4 * b) = o;
-                }
-            }
-        }
+        for (int pair = 0; pair < PAIRS; ++pair) put(pair / TB, pair % TB, acc[pair / TB][pair % TB]);
         return;
     }
-    // h in place of the gate's sums; the largest magnitude of a token's 128 columns over lanes and waves
-    const bool in = col < N;
+    __syncthreads();                                                   // every ring is done with: the parts take its place
+    float *red = reinterpret_cast<float *>(ring);                      // [wave][pair of blocks][lane], four at a time
 #pragma unroll
-    for (int i = 0; i < TB; ++i) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int b = 0; b < HB; ++b)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float h = in ? silu(acc[b][i][v]) * acc[HB + b < WB ? HB + b : 0][i][v] : 0.0f;
-                acc[b][i][v] = h;
-                m = max(m, __builtin_bit_cast(uint32_t, h) & 0x7fffffffu);
-            }
-        m = max(m, (uint32_t)__shfl_xor((int)m, 16, WAVE));
-        m = max(m, (uint32_t)__shfl_xor((int)m, 32, WAVE));
-        if (q4 == 0) s_amax[wn][wm * (TB * 16) + i * 16 + l16] = __builtin_bit_cast(float, m);
-    }
+    for (int pair = 0; pair < PAIRS; ++pair) *reinterpret_cast<f32x4 *>(red + ((wave * PAIRS + pair) * 64 + lane) * 4) = acc[pair / TB][pair % TB];
     __syncthreads();
+    for (int pair = wk; pair < PAIRS; pair += WK) {
+        f32x4 sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < TB; ++i) {
-        const int r = wm * (TB * 16) + i * 16 + l16;
-        uint32_t m = 0;
-#pragma unroll
-        for (int w = 0; w < WNN; ++w) m = max(m, __builtin_bit_cast(uint32_t, s_amax[w][r]));
-        if (row0 + r >= row_end) continue;
-        const float s = block_scale(m), inv = 1.0f / s;
-        if (wn == 0 && q4 == 0) p.c_scale[(size_t)(row0 + r) * nb_n + n0 / SCALE_BLOCK] = s;
-        if (!in) continue;
-        uint8_t *c = static_cast<uint8_t *>(p.c) + (size_t)(row0 + r) * N + col;
-#pragma unroll
-        for (int b = 0; b < HB; ++b)
-            *(BM_GLOBAL uint32_t *)(c + 4 * b) = e4m3x4(quotient(acc[b][i][0], s, inv), quotient(acc[b][i][1], s, inv),
-                                                        quotient(acc[b][i][2], s, inv), quotient(acc[b][i][3], s, inv));
+        for (int k = 0; k < WK; ++k) sum += *reinterpret_cast<const f32x4 *>(red + (((k * WR + wr) * PAIRS + pair) * 64 + lane) * 4);
+        put(pair / TB, pair % TB, sum);
     }
 }
 
-// Workgroups of a launch: a bound on the row tiles of any grouping of the rows, times the column tiles.
-static unsigned product_grid(const ProductParams &p, int bm, int cols) {
-    const long long groups = p.n_groups < p.rows ? p.n_groups : p.rows;
-    const long long tiles = (p.rows / bm + groups) * ((p.N + cols - 1) / cols);
-    return (unsigned)((tiles + 7) / 8 * 8);
+template <int WR, int WK, bool WIDE>
+__global__ void __launch_bounds__(WR * WK * 64, 2) stream_kernel(ProductParams p, int bm) {
+    constexpr int COLS = 32 * WR;
+    static_assert(SCALE_BLOCK % COLS == 0, "a tile's columns: one block of scales");
+    constexpr int RING = WR * WK * 4 * 4096, MAX_KB = MAX_PRODUCT_KD / SCALE_BLOCK;
+    __shared__ __attribute__((aligned(1024))) uint8_t ring[RING + (MAX_KB + STREAM_SCALES) * 4];
+    float *const s_sw = reinterpret_cast<float *>(ring + RING), *const s_sa = s_sw + MAX_KB;
+    TileTable &tt = *reinterpret_cast<TileTable *>(ring);                   // gone when the ring is filled
+    if (threadIdx.x < WAVE) build_tile_table(p, bm, tt);
+    __syncthreads();
+    const int n_nt = (p.N + COLS - 1) / COLS;
+    const Share share = my_share(__builtin_amdgcn_readfirstlane(tt.first[p.n_groups]) * n_nt);
+    if (share.begin >= share.end) return;
+    const Tile t = tile_at(p, tt, bm, n_nt, share.begin);
+    const Matrices m = matrices_of<false>(p, t.group);
+    const int rows = min(t.row_end - t.row0, bm), kb_n = (p.Kd + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    for (int kb = threadIdx.x; kb < kb_n; kb += WR * WK * 64) s_sw[kb] = ldg_f32(m.s0 + (size_t)(t.nt * COLS / SCALE_BLOCK) * kb_n + kb);
+    for (int r = threadIdx.x >> 6; r < rows; r += WR * WK) {
+        const float *src = p.a_scale + (size_t)source_row(p, t.row0 + r, t.row_end) * kb_n;
+        for (int k = threadIdx.x & 63; k < kb_n; k += 64) s_sa[r * kb_n + k] = ldg_f32(src + k);
+    }
+    __syncthreads();
+    if (rows <= 16) stream_tile<1, WR, WK, 4, WIDE>(p, t, rows, ring, s_sw, s_sa, m.w0);
+    else stream_tile<2, WR, WK, 4, WIDE>(p, t, rows, ring, s_sw, s_sa, m.w0);
+}
+
+// A bound on the row tiles of any grouping of the rows, times the column tiles.
+static long long tiles_bound(long long rows, int N, int n_groups, int bm, int cols) {
+    const long long groups = n_groups < rows ? n_groups : rows;
+    return (rows / bm + groups) * ((N + cols - 1) / cols);
+}
+
+static bool near(const ProductParams &p) {
+    return p.Kd % SCALE_BLOCK == 0 && p.Kd >= 4 * SCALE_BLOCK && (long long)p.a_rows * p.Kd < (1ll << 32);
 }
 
 bool product_grid_ok(long long rows, int N, int n_groups) {
-    return (rows / 16 + n_groups) * ((N + 31) / 32) < (1ll << 31) - 8;       // no tile is smaller
+    return tiles_bound(rows, N, n_groups, 8, 32) < (1ll << 31) - 8;       // no tile is smaller
 }
 
-template <int BM, int BN, int NW, int WNN, int S, bool DUAL, bool WIDE>
+template <int BM, int WNN, int SW, int ST, int PER_UNIT, bool DUAL, bool WIDE, bool NEAR>
 static void launch_tiles(const ProductParams &p, hipStream_t st) {
-    hipLaunchKernelGGL((product_kernel<BM, BN, NW, WNN, S, DUAL, WIDE>), dim3(product_grid(p, BM, DUAL ? BN / 2 : BN)), dim3(NW * 64), 0, st, p);
+    const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, BM, DUAL ? 128 : 256) + 7) / 8 * 8;
+    hipLaunchKernelGGL((tiles_kernel<BM, WNN, SW, ST, PER_UNIT, DUAL, WIDE, NEAR>), dim3((unsigned)(tiles < 256 * PER_UNIT ? tiles : 256 * PER_UNIT)), dim3(512), 0, st, p);
+}
+
+template <bool DUAL, bool WIDE>
+static void launch_large_tiles(const ProductParams &p, hipStream_t st) {
+    if (near(p)) launch_tiles<192, 4, 3, 2, 1, DUAL, WIDE, true>(p, st);
+    else launch_tiles<128, 4, 3, 3, 1, DUAL, WIDE, false>(p, st);
+}
+
+template <int WR, int WK, bool WIDE>
+static void launch_stream(const ProductParams &p, hipStream_t st) {
+    const int kb_n = (p.Kd + SCALE_BLOCK - 1) / SCALE_BLOCK, bm = 32 * kb_n <= STREAM_SCALES ? 32 : 8;
+    const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, bm, 32 * WR) + 7) / 8 * 8;
+    hipLaunchKernelGGL((stream_kernel<WR, WK, WIDE>), dim3((unsigned)tiles), dim3(WR * WK * 64), 0, st, p, bm);
+}
+
+template <bool WIDE>
+static void launch_product_t(const ProductParams &p, hipStream_t st) {
+    const long long avg = p.rows / p.n_groups;
+    if (avg >= 128) launch_large_tiles<false, WIDE>(p, st);
+    else if (p.Kd >= 2048) launch_stream<1, 4, WIDE>(p, st);
+    else launch_stream<4, 1, WIDE>(p, st);
 }
 
 int launch_product(const ProductParams &p, hipStream_t st) {
-    const long long avg = p.rows / p.n_groups;
-    if (p.c_f32) {
-        if (avg >= 128) launch_tiles<256, 256, 8, 4, 2, false, true>(p, st);
-        else launch_tiles<64, 64, 4, 4, 4, false, true>(p, st);
-    } else {
-        if (avg >= 128) launch_tiles<256, 256, 8, 4, 2, false, false>(p, st);
-        else launch_tiles<64, 64, 4, 4, 4, false, false>(p, st);
-    }
+    if (p.c_f32) launch_product_t<true>(p, st);
+    else launch_product_t<false>(p, st);
     return launch_status(__func__);
 }
 
 int launch_swiglu(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
-    if (avg >= 128) launch_tiles<256, 256, 8, 4, 2, true, true>(p, st);
-    else launch_tiles<64, 256, 8, 8, 3, true, true>(p, st);
+    if (avg >= 128) launch_large_tiles<true, true>(p, st);
+    else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= 512) {
+        if (near(p)) launch_tiles<32, 8, 4, 4, 1, true, true, true>(p, st);
+        else launch_tiles<32, 8, 4, 4, 1, true, true, false>(p, st);
+    } else {
+        if (near(p)) launch_tiles<32, 8, 2, 2, 2, true, true, true>(p, st);
+        else launch_tiles<32, 8, 2, 2, 2, true, true, false>(p, st);
+    }
     return launch_status(__func__);
 }
 

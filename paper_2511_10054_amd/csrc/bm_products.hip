@@ -200,7 +200,7 @@ __device__ uint4 zero_piece;             // where pieces of tokens past the row'
 }  // namespace
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Tiles of BM tokens x 256 weight rows (DUAL: 128 of the gate, 128 of the up matrix) on 8 waves, WNN of them along the weight
+// Tiles of BM tokens x BN weight rows (DUAL: 128 of the gate, 128 of the up matrix) on 8 waves, WNN of them along the weight
 // rows.  The reduction goes in steps of 128 through two rings in LDS, SW stages of weights and ST of tokens, filled with
 // direct loads: a row's 128 bytes are one cache line, 8 rows an instruction.  Piece p of row r lies in slot p ^ ((r >> 1) & 7),
 // so that the 16 rows of an operand read fall into different banks.
@@ -216,9 +216,9 @@ __device__ uint4 zero_piece;             // where pieces of tokens past the row'
 // Everything lies in one LDS array: of several, the compiler tells apart which one direct loads fill, and holds every read
 // of that one until no load is in flight.
 // ---------------------------------------------------------------------------------------------------------------------
-template <int BM, int WNN, int SW, int ST, int PER_UNIT, bool DUAL, bool WIDE, bool NEAR>
-__global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams p) {
-    constexpr int NW = 8, BN = 256, WMN = NW / WNN;
+template <int BM, int BN, int WMN, int WNN, int KG, int SW, int ST, int PER_UNIT, bool DUAL, bool WIDE, bool NEAR>
+__global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT / 4) tiles_kernel(ProductParams p) {
+    constexpr int NW = WMN * WNN;                              // waves of each of the KG parts of the reduction
     constexpr int TB = BM / WMN / 16, WB = BN / WNN / 16;      // 16-token and 16-row blocks of a wave
     constexpr int HB = DUAL ? WB / 2 : WB;                     // of these, blocks of different columns
     constexpr int COLS = DUAL ? BN / 2 : BN;
@@ -231,21 +231,22 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
     static_assert(TB * 16 * WMN == BM && WB * 16 * WNN == BN && (TR >= 8 ? TR % 8 == 0 : TR > 0), "tile shape");
     static_assert(ST <= SW && SW <= MIN_STEPS && AHEAD < 64, "stages");
     constexpr int MAX_KB = MAX_PRODUCT_KD / SCALE_BLOCK;
-    constexpr int W_BYTES = SW * BN * 128, T_BYTES = ST * BM * 128;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[W_BYTES + T_BYTES + (ST * BM + 4 * MAX_KB + BM + (DUAL ? WNN * BM : 0)) * 4 + sizeof(TileTable)];
+    constexpr int W_BYTES = SW * KG * BN * 128, T_BYTES = ST * KG * BM * 128, EXCHANGE = KG > 1 ? (KG - 1) * NW * 1024 : 0;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[W_BYTES + T_BYTES + EXCHANGE + (ST * KG * BM + 4 * MAX_KB + BM + (DUAL ? WNN * BM : 0)) * 4 + sizeof(TileTable)];
     uint8_t *const w_ring = lds, *const t_ring = lds + W_BYTES;
-    float *const s_sa = reinterpret_cast<float *>(t_ring + T_BYTES);              // [ST][BM] tokens' scales
-    float *const s_sw = s_sa + ST * BM;                                           // [2 tiles][2][MAX_KB] weight blocks' scales
+    f32x4 *const s_part = reinterpret_cast<f32x4 *>(t_ring + T_BYTES);            // [KG - 1][NW][64] sums on their way to the first part
+    float *const s_sa = reinterpret_cast<float *>(t_ring + T_BYTES + EXCHANGE);   // [ST][KG][BM] tokens' scales
+    float *const s_sw = s_sa + ST * KG * BM;                                           // [2 tiles][2][MAX_KB] weight blocks' scales
     int *const s_id = reinterpret_cast<int *>(s_sw + 4 * MAX_KB);                 // [BM] row_map of the next tile
     uint32_t *const s_amax = reinterpret_cast<uint32_t *>(s_id + BM);             // [WNN][BM]
     TileTable &tt = *reinterpret_cast<TileTable *>(s_amax + (DUAL ? WNN * BM : 0));
 
-    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = lane_id(), all = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), kg = all / NW, wave = all % NW;
     const int wm = wave / WNN, wn = wave % WNN, q4 = lane >> 4, l16 = lane & 15;
     const int N = p.N, Kd = p.Kd, kb_n = (Kd + SCALE_BLOCK - 1) / SCALE_BLOCK, nb_n = (N + SCALE_BLOCK - 1) / SCALE_BLOCK;
-    const int n_nt = (N + COLS - 1) / COLS, KT = NEAR ? kb_n : max(kb_n, MIN_STEPS);
+    const int n_nt = (N + COLS - 1) / COLS, KT = NEAR ? kb_n / KG : max((kb_n + KG - 1) / KG, MIN_STEPS);
 
-    if (wave == 0) build_tile_table(p, BM, tt);
+    if (all == 0) build_tile_table(p, BM, tt);
     BM_WAIT_AND_MEET(0)
     const Share share = my_share(__builtin_amdgcn_readfirstlane(tt.first[p.n_groups]) * n_nt);
     if (share.begin >= share.end) return;
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
     auto w_piece = [&](int j) { return (lane & 7) ^ (((wave * (WI * 8) + j * 8 + (lane >> 3)) >> 1) & 7); };
     auto t_pos = [&](int j) { return wave * TR + j * 8 + (TR >= 8 ? lane >> 3 : min(lane >> 3, TR - 1)); };
     auto t_piece = [&](int j) { return (lane & 7) ^ ((t_pos(j) >> 1) & 7); };
-    auto entry_of = [&](const Tile &t) { return BM <= 64 && kb_n >= MIN_STEPS ? entry_block(t, kb_n) : 0; };
+    auto entry_of = [&](const Tile &t) { return BM <= 64 ? entry_block(t, KT) : 0; };
     auto aim_weights = [&](const Tile &t) {
         const int n0 = t.nt * COLS;
         wt = matrices_of<DUAL>(p, t.group);
@@ -292,11 +293,11 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
         else sp = p.a_scale + (size_t)row(wave * TR + min(lane, TR - 1)) * kb_n;
         t_entry = entry_of(t);
     };
-    auto block_at = [&](int step, int entry) { return step + entry < KT ? step + entry : step + entry - KT; };
+    auto block_at = [&](int step, int entry) { return (step + entry < KT ? step + entry : step + entry - KT) * KG + kg; };
     // Pieces past the row's end: of weights any piece of the row, of tokens zeros.  Blocks past the last one: the first, and zeros.
     auto load_weights = [&](int step, int slot) {
         const int kt = block_at(step, w_entry), k0 = NEAR || kt < kb_n ? kt * 128 : 0;
-        uint8_t *base = w_ring + slot * (BN * 128);
+        uint8_t *base = w_ring + (slot * KG + kg) * (BN * 128);
 #pragma unroll
         for (int j = 0; j < WI; ++j) {
             const int pos = wave * (WI * 8) + j * 8, pc = w_piece(j) * 16;
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
     };
     auto load_tokens = [&](int step, int slot) {
         const int kt = block_at(step, t_entry), k0 = kt * 128;
-        uint8_t *base = t_ring + slot * (BM * 128);
+        uint8_t *base = t_ring + (slot * KG + kg) * (BM * 128);
 #pragma unroll
         for (int j = 0; j < TI; ++j) {
             const uint8_t *src;
@@ -320,15 +321,15 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
         if constexpr (NEAR) sc = p.a_scale + kt + so;
         else sc = sp + min(kt, kb_n - 1);
         if (lane < TR)
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)sc, (BM_LDS void *)(s_sa + slot * BM + wave * TR), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)sc, (BM_LDS void *)(s_sa + (slot * KG + kg) * BM + wave * TR), 4, 0, 0);
     };
     // What a tile needs beside its operands: the scales of its weight blocks (a wave fetches 64 of one of two rows) and its rows' ids
     auto load_meta = [&](const Tile &t, int buf, bool ids) {
-        const int j = wave >> 2, kb = (wave & 3) * 64 + lane, nb = min(t.nt * COLS / SCALE_BLOCK + (DUAL ? 0 : j), nb_n - 1);
+        const int j = all >> 2, kb = (all & 3) * 64 + lane, nb = min(t.nt * COLS / SCALE_BLOCK + (DUAL ? 0 : j), nb_n - 1);
         const Matrices m = matrices_of<DUAL>(p, t.group);
         const float *s = (DUAL && j ? m.s1 : m.s0) + (size_t)nb * kb_n;
-        if (kb < kb_n)
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(s + kb), (BM_LDS void *)(s_sw + (buf * 2 + j) * MAX_KB + (wave & 3) * 64), 4, 0, 0);
+        if (j < 2 && kb < kb_n)
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(s + kb), (BM_LDS void *)(s_sw + (buf * 2 + j) * MAX_KB + (all & 3) * 64), 4, 0, 0);
         if (ids && p.row_map && lane < TR)
             __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(p.row_map + min(t.row0 + wave * TR + lane, t.row_end - 1)),
                                              (BM_LDS void *)(s_id + wave * TR), 4, 0, 0);
@@ -375,8 +376,8 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
                 load_weights(step + SW - 1 < KT ? step + SW - 1 : step + SW - 1 - KT, w_slot);
                 advance(w_slot, SW);
             }
-            const uint8_t *ws = w_ring + w_read * (BN * 128), *ts = t_ring + t_read * (BM * 128);
-            const float *sa_at = s_sa + t_read * BM + wm * (TB * 16) + l16;
+            const uint8_t *ws = w_ring + (w_read * KG + kg) * (BN * 128), *ts = t_ring + (t_read * KG + kg) * (BM * 128);
+            const float *sa_at = s_sa + (t_read * KG + kg) * BM + wm * (TB * 16) + l16;
             const int kt = NEAR ? block_at(step, entry) : min(block_at(step, entry), kb_n - 1);
             // DUAL: the gate's and the up matrix's scale; else one of the two blocks of 128 columns, the wave's
             const float sw0 = s_sw[(buf * 2 + (DUAL ? 0 : wn * (16 * HB) / SCALE_BLOCK)) * MAX_KB + kt];
@@ -422,13 +423,27 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
             advance(t_read, ST);
         }
 
+        // the parts of the reduction, added in order: one block of 16 x 16 of every wave at a time
+        if constexpr (KG > 1) {
+#pragma unroll
+            for (int i = 0; i < TB; ++i)
+#pragma unroll
+                for (int b = 0; b < WB; ++b) {
+                    if (kg > 0) s_part[((kg - 1) * NW + wave) * 64 + lane] = acc[b][i];
+                    BM_WAIT_AND_MEET(63)
+                    if (kg == 0)
+#pragma unroll
+                        for (int k = 0; k < KG - 1; ++k) acc[b][i] += s_part[(k * NW + wave) * 64 + lane];
+                    BM_WAIT_AND_MEET(63)
+                }
+        }
         // ---- write-out: a lane holds 4 * HB consecutive columns of each of its tokens (N is a multiple of 32: all in or none) ----
         const int n0 = cur.nt * COLS, col = n0 + wn * (16 * HB) + q4 * (4 * HB), first = wm * (TB * 16) + l16;
         if constexpr (!DUAL) {
 #pragma unroll
             for (int i = 0; i < TB; ++i) {
                 const int r = cur.row0 + first + i * 16;
-                if (r >= cur.row_end || col >= N) continue;
+                if (kg > 0 || r >= cur.row_end || col >= N) continue;
 #pragma unroll
                 for (int b = 0; b < WB; ++b) store4(p, (size_t)r * N + col + 4 * b, acc[b][i]);
             }
@@ -449,7 +464,7 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
                     }
                 m = max(m, (uint32_t)__shfl_xor((int)m, 16, WAVE));
                 m = max(m, (uint32_t)__shfl_xor((int)m, 32, WAVE));
-                if (q4 == 0) s_amax[wn * BM + first + i * 16] = m;
+                if (q4 == 0 && kg == 0) s_amax[wn * BM + first + i * 16] = m;
             }
             BM_WAIT_AND_MEET(63)                              // LDS only: loads go on
 #pragma unroll
@@ -458,7 +473,7 @@ __global__ void __launch_bounds__(512, 2 * PER_UNIT) tiles_kernel(ProductParams 
                 uint32_t m = 0;
 #pragma unroll
                 for (int w = 0; w < WNN; ++w) m = max(m, s_amax[w * BM + at]);
-                if (r >= cur.row_end) continue;
+                if (kg > 0 || r >= cur.row_end) continue;
                 const float s = block_scale(m), inv = 1.0f / s;
                 if (wn == 0 && q4 == 0) p.c_scale[(size_t)r * nb_n + cur.nt] = s;
                 if (!in) continue;
@@ -630,39 +645,37 @@ static long long tiles_bound(long long rows, int N, int n_groups, int bm, int co
     return (rows / bm + groups) * ((N + cols - 1) / cols);
 }
 
-static bool near(const ProductParams &p) {
-    return p.Kd % SCALE_BLOCK == 0 && p.Kd >= 4 * SCALE_BLOCK && (long long)p.a_rows * p.Kd < (1ll << 32);
-}
-
 bool product_grid_ok(long long rows, int N, int n_groups) {
     return tiles_bound(rows, N, n_groups, 8, 32) < (1ll << 31) - 8;       // no tile is smaller
 }
 
-template <int BM, int WNN, int SW, int ST, int PER_UNIT, bool DUAL, bool WIDE, bool NEAR>
+template <int BM, int BN, int WMN, int WNN, int KG, int SW, int ST, int PER_UNIT, bool DUAL, bool WIDE>
 static void launch_tiles(const ProductParams &p, hipStream_t st) {
-    const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, BM, DUAL ? 128 : 256) + 7) / 8 * 8;
-    hipLaunchKernelGGL((tiles_kernel<BM, WNN, SW, ST, PER_UNIT, DUAL, WIDE, NEAR>), dim3((unsigned)(tiles < 256 * PER_UNIT ? tiles : 256 * PER_UNIT)), dim3(512), 0, st, p);
+    const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, BM, DUAL ? BN / 2 : BN) + 7) / 8 * 8;
+    const dim3 grid((unsigned)(tiles < 256 * PER_UNIT ? tiles : 256 * PER_UNIT)), block(WMN * WNN * KG * 64);
+    // 32-bit offsets into a, whole steps (see tiles_kernel)
+    const bool near = p.Kd % (KG * SCALE_BLOCK) == 0 && p.Kd >= 4 * KG * SCALE_BLOCK && (long long)p.a_rows * p.Kd < (1ll << 32);
+    if (near) hipLaunchKernelGGL((tiles_kernel<BM, BN, WMN, WNN, KG, SW, ST, PER_UNIT, DUAL, WIDE, true>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((tiles_kernel<BM, BN, WMN, WNN, KG, SW, ST, PER_UNIT, DUAL, WIDE, false>), grid, block, 0, st, p);
 }
 
-template <bool DUAL, bool WIDE>
-static void launch_large_tiles(const ProductParams &p, hipStream_t st) {
-    if (near(p)) launch_tiles<192, 4, 3, 2, 1, DUAL, WIDE, true>(p, st);
-    else launch_tiles<128, 4, 3, 3, 1, DUAL, WIDE, false>(p, st);
-}
-
-template <int WR, int WK, bool WIDE>
+template <bool WIDE>
 static void launch_stream(const ProductParams &p, hipStream_t st) {
     const int kb_n = (p.Kd + SCALE_BLOCK - 1) / SCALE_BLOCK, bm = 32 * kb_n <= STREAM_SCALES ? 32 : 8;
-    const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, bm, 32 * WR) + 7) / 8 * 8;
-    hipLaunchKernelGGL((stream_kernel<WR, WK, WIDE>), dim3((unsigned)tiles), dim3(WR * WK * 64), 0, st, p, bm);
+    const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, bm, 32) + 7) / 8 * 8;
+    hipLaunchKernelGGL((stream_kernel<1, 4, WIDE>), dim3((unsigned)tiles), dim3(256), 0, st, p, bm);
 }
 
 template <bool WIDE>
 static void launch_product_t(const ProductParams &p, hipStream_t st) {
-    const long long avg = p.rows / p.n_groups;
-    if (avg >= 128) launch_large_tiles<false, WIDE>(p, st);
-    else if (p.Kd >= 2048) launch_stream<1, 4, WIDE>(p, st);
-    else launch_stream<4, 1, WIDE>(p, st);
+    const long long avg = p.rows / p.n_groups;                // (groups of experts that are not resident are empty: the live ones have more)
+    auto tiles = [&](int bm, int bn) { return tiles_bound(p.rows, p.N, p.n_groups, bm, bn); };
+    if (avg >= 256 && tiles(192, 256) >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, false, WIDE>(p, st);
+    else if (avg >= 48 && tiles(128, 128) >= 256) launch_tiles<128, 128, 2, 4, 1, 2, 2, 2, false, WIDE>(p, st);
+    else if (avg >= (p.Kd >= 2048 ? 32 : 16) && tiles(64, 128) >= 256) launch_tiles<64, 128, 2, 4, 1, 3, 3, 2, false, WIDE>(p, st);
+    else if (p.Kd >= 2048 && tiles(32, 128) <= 128) launch_stream<WIDE>(p, st);
+    else if (p.Kd >= 2048) launch_tiles<32, 128, 1, 4, 2, 3, 3, 1, false, WIDE>(p, st);
+    else launch_tiles<32, 128, 2, 4, 1, 3, 3, 2, false, WIDE>(p, st);
 }
 
 int launch_product(const ProductParams &p, hipStream_t st) {
@@ -673,14 +686,10 @@ int launch_product(const ProductParams &p, hipStream_t st) {
 
 int launch_swiglu(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
-    if (avg >= 128) launch_large_tiles<true, true>(p, st);
-    else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= 512) {
-        if (near(p)) launch_tiles<32, 8, 4, 4, 1, true, true, true>(p, st);
-        else launch_tiles<32, 8, 4, 4, 1, true, true, false>(p, st);
-    } else {
-        if (near(p)) launch_tiles<32, 8, 2, 2, 2, true, true, true>(p, st);
-        else launch_tiles<32, 8, 2, 2, 2, true, true, false>(p, st);
-    }
+    if (avg >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, true, true>(p, st);
+    else if (avg >= 96) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, true, true>(p, st);
+    else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= 512) launch_tiles<32, 256, 1, 8, 1, 4, 4, 1, true, true>(p, st);
+    else launch_tiles<32, 256, 1, 8, 1, 2, 2, 2, true, true>(p, st);
     return launch_status(__func__);
 }
 

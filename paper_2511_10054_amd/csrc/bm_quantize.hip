@@ -97,22 +97,68 @@ __device__ __forceinline__ void store_q8(uint8_t *p, int n, const float (&v)[8],
 
 }  // namespace
 
+// Eight consecutive values as they lie in memory: 16-bit ones stay packed until they are converted (half the registers, and
+// their largest magnitude is found two at a time on the bits).
+template <typename T> struct Piece {
+    float v[8];
+    template <bool ALIGNED> __device__ __forceinline__ void load(const float *p, int n) { load8<ALIGNED>(p, n, v); }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    }
+    __device__ __forceinline__ uint32_t max_of() const { return max_bits(v, 0); }
+    __device__ __forceinline__ void get(float (&o)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = v[i];
+    }
+};
+template <> struct Piece<uint16_t> {
+    u32x4 u;
+    template <bool ALIGNED> __device__ __forceinline__ void load(const uint16_t *p, int n) {
+        if (ALIGNED) {
+            u = ldg128(p);
+        } else {
+            clear();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) u[i / 2] |= (uint32_t)*(const BM_GLOBAL uint16_t *)(p + i) << (16 * (i & 1));
+        }
+    }
+    __device__ __forceinline__ void clear() { u = u32x4{0u, 0u, 0u, 0u}; }
+    __device__ __forceinline__ uint32_t max_of() const {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        auto mag = [&](int i) { return __builtin_bit_cast(u16x2, u[i] & 0x7fff7fffu); };
+        const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(0), mag(1)), __builtin_elementwise_max(mag(2), mag(3)));
+        return (uint32_t)max(m[0], m[1]) << 16;
+    }
+    __device__ __forceinline__ void get(float (&o)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            o[2 * i] = __builtin_bit_cast(float, u[i] << 16);
+            o[2 * i + 1] = __builtin_bit_cast(float, u[i] & 0xffff0000u);
+        }
+    }
+};
+
 // ---------------------------------------------------------------------------------------------------------------------
 // A scale for each 128 values of a row: 16 lanes of eight values each hold a block.
 // ---------------------------------------------------------------------------------------------------------------------
 template <bool ALIGNED, typename T>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *src, uint8_t *q, float *scale, long long n_rows, int cols, int kb) {
     const long long blk = (long long)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const long long row = blk / kb;
+    const long long row = n_rows * kb < (1ll << 32) ? (uint32_t)blk / (uint32_t)kb : blk / kb;
     const int j = (int)(blk - row * kb) * SCALE_BLOCK + (threadIdx.x & 15) * 8;
     const bool in = row < n_rows && j < cols;
-    float v[8] = {};
+    Piece<T> v;
+    v.clear();
     const long long at = row * cols + j;
-    if (in) load8<ALIGNED>(src + at, cols - j, v);
-    const uint32_t m = row16_max_u32(max_bits(v, 0));
+    if (in) v.template load<ALIGNED>(src + at, cols - j);
+    const uint32_t m = row16_max_u32(v.max_of());
     if (!in) return;
     const float s = block_scale(m), inv = 1.0f / s;
-    store_q8<ALIGNED>(q + at, cols - j, v, s, inv);
+    float f[8];
+    v.get(f);
+    store_q8<ALIGNED>(q + at, cols - j, f, s, inv);
     if ((threadIdx.x & 15) == 0) scale[blk] = s;
 }
 
@@ -126,18 +172,16 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const T *src, uint
     const int tid = threadIdx.x;
     const int j = blockIdx.x * SCALE_BLOCK + (tid & 15) * 8, r0 = blockIdx.y * SCALE_BLOCK + (tid >> 4);
     const size_t base = (size_t)blockIdx.z * rows * cols;
-    float v[8][8];
+    Piece<T> v[8];
     uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = r0 + 16 * i;
-        if (r < rows && j < cols) load8<ALIGNED>(src + base + (size_t)r * cols + j, cols - j, v[i]);
-        else
-#pragma unroll
-            for (int u = 0; u < 8; ++u) v[i][u] = 0.0f;
+        v[i].clear();
+        if (r < rows && j < cols) v[i].template load<ALIGNED>(src + base + (size_t)r * cols + j, cols - j);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max_bits(v[i], m);
+    for (int i = 0; i < 8; ++i) m = max(m, v[i].max_of());
     m = wave_max_u32(m);
     if ((tid & 63) == 0) s_max[tid >> 6] = m;
     __syncthreads();
@@ -146,7 +190,9 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const T *src, uint
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = r0 + 16 * i;
-        if (r < rows && j < cols) store_q8<ALIGNED>(q + base + (size_t)r * cols + j, cols - j, v[i], s, inv);
+        float f[8];
+        v[i].get(f);
+        if (r < rows && j < cols) store_q8<ALIGNED>(q + base + (size_t)r * cols + j, cols - j, f, s, inv);
     }
     if (tid == 0) scale[((size_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x] = s;
 }

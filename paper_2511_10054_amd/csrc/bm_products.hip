@@ -20,6 +20,9 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // Eight e4m3 values as fp16 (exact: three mantissa bits, exponents down to 2^-9)
+__device__ __forceinline__ f16x2 widen2(uint32_t a, bool high) {
+    return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
+}
 __device__ __forceinline__ f16x8 widen8(int a, int b) {
     const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
     const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
@@ -162,6 +165,9 @@ __device__ __forceinline__ int source_row(const ProductParams &p, int row, int r
 }
 
 // A lane's 32 values of row pos of a stage: pieces q4 and q4 + 4 (any order serves, the same for both operands)
+__device__ __forceinline__ u32x4 lds_piece(const uint8_t *rows, int pos, int piece) {
+    return *reinterpret_cast<const u32x4 *>(rows + pos * 128 + ((piece ^ ((pos >> 1) & 7)) * 16));
+}
 __device__ __forceinline__ i32x8 lds_operand(const uint8_t *rows, int pos, int q4) {
     const int x = (pos >> 1) & 7;
     const u32x4 lo = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + ((q4 ^ x) * 16));
@@ -227,6 +233,8 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
     constexpr int PER = WI + TI + 1;                           // with the tokens' scales
     constexpr int AHEAD = ST < SW ? WI + (ST - 2) * PER : (ST - 2) * PER;
     constexpr int PART = BM <= 64 ? 1 : TB;                    // blocks that are multiplied or, where no token is theirs, left out together
+    constexpr bool SPREAD = BM > 64 && PER_UNIT == 1;           // loads are issued between the matrix instructions
+    static_assert(!SPREAD || PER <= TB * WB / 2, "places for loads");
     constexpr int MIN_STEPS = 4;                               // shorter walks are filled up with blocks of zeros
     static_assert(TB * 16 * WMN == BM && WB * 16 * WNN == BN && (TR >= 8 ? TR % 8 == 0 : TR > 0), "tile shape");
     static_assert(ST <= SW && SW <= MIN_STEPS && AHEAD < 64, "stages");
@@ -278,50 +286,52 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
             wo[j] = (uint32_t)n * (uint32_t)Kd + w_piece(j) * 16;
         }
     };
-    // rows by their ids in LDS (row r of the tile at s_id[r]), or by row_map
+    // a lane finds one of its wave's rows: by its id in LDS (row r of the tile at s_id[r]), or by row_map
     auto aim_tokens = [&](const Tile &t, bool ids) {
-        auto row = [&](int pos) {
-            if (!ids || !p.row_map) return source_row(p, t.row0 + pos, t.row_end);
-            return row_of_id(p, s_id[pos]);
-        };
+        const int mine = wave * TR + min(lane, TR - 1);
+        const int row = ids && p.row_map ? row_of_id(p, s_id[mine]) : source_row(p, t.row0 + mine, t.row_end);
 #pragma unroll
         for (int j = 0; j < TI; ++j) {
-            if constexpr (NEAR) to[j] = (uint32_t)row(t_pos(j)) * (uint32_t)Kd + t_piece(j) * 16;
-            else tp[j] = p.a + (size_t)row(t_pos(j)) * Kd + t_piece(j) * 16;
+            const int r = __shfl(row, t_pos(j) - wave * TR, WAVE);
+            if constexpr (NEAR) to[j] = (uint32_t)r * (uint32_t)Kd + t_piece(j) * 16;
+            else tp[j] = p.a + (size_t)r * Kd + t_piece(j) * 16;
         }
-        if constexpr (NEAR) so = (uint32_t)row(wave * TR + min(lane, TR - 1)) * (uint32_t)kb_n;
-        else sp = p.a_scale + (size_t)row(wave * TR + min(lane, TR - 1)) * kb_n;
+        if constexpr (NEAR) so = (uint32_t)row * (uint32_t)kb_n;
+        else sp = p.a_scale + (size_t)row * kb_n;
         t_entry = entry_of(t);
     };
     auto block_at = [&](int step, int entry) { return (step + entry < KT ? step + entry : step + entry - KT) * KG + kg; };
     // Pieces past the row's end: of weights any piece of the row, of tokens zeros.  Blocks past the last one: the first, and zeros.
-    auto load_weights = [&](int step, int slot) {
+    auto load_weight = [&](int step, int slot, int j) {
         const int kt = block_at(step, w_entry), k0 = NEAR || kt < kb_n ? kt * 128 : 0;
-        uint8_t *base = w_ring + (slot * KG + kg) * (BN * 128);
-#pragma unroll
-        for (int j = 0; j < WI; ++j) {
-            const int pos = wave * (WI * 8) + j * 8, pc = w_piece(j) * 16;
-            const uint8_t *from = (DUAL && (pos >> 4) % WB >= HB ? wt.w1 : wt.w0) + k0;
-            const uint32_t off = NEAR || k0 + pc < Kd ? wo[j] : wo[j] - pc;
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(from + off), (BM_LDS void *)(base + pos * 128), 16, 0, 0);
-        }
+        const int pos = wave * (WI * 8) + j * 8, pc = w_piece(j) * 16;
+        const uint8_t *from = (DUAL && (pos >> 4) % WB >= HB ? wt.w1 : wt.w0) + k0;
+        const uint32_t off = NEAR || k0 + pc < Kd ? wo[j] : wo[j] - pc;
+        __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(from + off), (BM_LDS void *)(w_ring + (slot * KG + kg) * (BN * 128) + pos * 128), 16, 0, 0);
     };
-    auto load_tokens = [&](int step, int slot) {
+    auto load_token = [&](int step, int slot, int j) {
         const int kt = block_at(step, t_entry), k0 = kt * 128;
-        uint8_t *base = t_ring + (slot * KG + kg) * (BM * 128);
-#pragma unroll
-        for (int j = 0; j < TI; ++j) {
+        if (j < TI) {
             const uint8_t *src;
             if constexpr (NEAR) src = p.a + k0 + to[j];
             else src = k0 + t_piece(j) * 16 < Kd ? tp[j] + k0 : reinterpret_cast<const uint8_t *>(&zero_piece);
             if (TR >= 8 || lane < TR * 8)
-                __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)(base + (wave * TR + j * 8) * 128), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)(t_ring + (slot * KG + kg) * (BM * 128) + (wave * TR + j * 8) * 128), 16, 0, 0);
+        } else {
+            const float *sc;
+            if constexpr (NEAR) sc = p.a_scale + kt + so;
+            else sc = sp + min(kt, kb_n - 1);
+            if (lane < TR)
+                __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)sc, (BM_LDS void *)(s_sa + (slot * KG + kg) * BM + wave * TR), 4, 0, 0);
         }
-        const float *sc;
-        if constexpr (NEAR) sc = p.a_scale + kt + so;
-        else sc = sp + min(kt, kb_n - 1);
-        if (lane < TR)
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)sc, (BM_LDS void *)(s_sa + (slot * KG + kg) * BM + wave * TR), 4, 0, 0);
+    };
+    auto load_weights = [&](int step, int slot) {
+#pragma unroll
+        for (int j = 0; j < WI; ++j) load_weight(step, slot, j);
+    };
+    auto load_tokens = [&](int step, int slot) {
+#pragma unroll
+        for (int j = 0; j <= TI; ++j) load_token(step, slot, j);
     };
     // What a tile needs beside its operands: the scales of its weight blocks (a wave fetches 64 of one of two rows) and its rows' ids
     auto load_meta = [&](const Tile &t, int buf, bool ids) {
@@ -360,20 +370,26 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
             for (int i = 0; i < TB; ++i) acc[b][i] = 0.0f;
 
         for (int step = 0; step < KT; ++step) {
-            if (more || step + SW - 2 < KT) BM_WAIT_AND_MEET(AHEAD)
+            if (SPREAD || more || step + SW - 2 < KT) BM_WAIT_AND_MEET(AHEAD)
             else BM_WAIT_AND_MEET(0)
             if (step == 0 && more) {
                 next = tile_at(p, tt, BM, n_nt, lid + share.step);
                 load_meta(next, buf ^ 1, true);
             }
-            if (step + ST - 1 < KT || more) {
-                if (step + ST - 1 == KT) aim_tokens(next, true);
-                load_tokens(step + ST - 1 < KT ? step + ST - 1 : step + ST - 1 - KT, t_slot);
+            if (more && step + ST - 1 == KT) aim_tokens(next, true);
+            if (more && step + SW - 1 == KT) aim_weights(next);
+            const int t_step = step + ST - 1 < KT ? step + ST - 1 : step + ST - 1 - KT, w_step = step + SW - 1 < KT ? step + SW - 1 : step + SW - 1 - KT;
+            const int t_fill = t_slot, w_fill = w_slot;
+            auto load_part = [&](int j) {
+                if (j <= TI) load_token(t_step, t_fill, j);
+                else if (j < PER) load_weight(w_step, w_fill, j - TI - 1);
+            };
+            if (SPREAD || more || step + ST - 1 < KT) {
+                if (!SPREAD) load_tokens(t_step, t_slot);
                 advance(t_slot, ST);
             }
-            if (step + SW - 1 < KT || more) {
-                if (step + SW - 1 == KT) aim_weights(next);
-                load_weights(step + SW - 1 < KT ? step + SW - 1 : step + SW - 1 - KT, w_slot);
+            if (SPREAD || more || step + SW - 1 < KT) {
+                if (!SPREAD) load_weights(w_step, w_slot);
                 advance(w_slot, SW);
             }
             const uint8_t *ws = w_ring + (w_read * KG + kg) * (BN * 128), *ts = t_ring + (t_read * KG + kg) * (BM * 128);
@@ -382,7 +398,66 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
             // DUAL: the gate's and the up matrix's scale; else one of the two blocks of 128 columns, the wave's
             const float sw0 = s_sw[(buf * 2 + (DUAL ? 0 : wn * (16 * HB) / SCALE_BLOCK)) * MAX_KB + kt];
             const float sw1 = DUAL ? s_sw[(buf * 2 + 1) * MAX_KB + kt] : sw0;
-            if (BM > 64 && live <= 0) { advance(w_read, SW); advance(t_read, ST); continue; }
+            if (BM > 64 && live <= 0) {
+                if (SPREAD) {
+                    load_tokens(t_step, t_fill);
+                    load_weights(w_step, w_fill);
+                }
+                advance(w_read, SW);
+                advance(t_read, ST);
+                continue;
+            }
+            if constexpr (WIDE && BM > 64) {
+                // Beside every matrix instruction stand the widening of the next 32 values of the tokens (in the first 16 tokens, of
+                // the weights too) and the addition of one result of the 16 tokens before: a unit takes a matrix instruction in 16
+                // cycles and the others of the same wave meanwhile
+                const int pos0 = wm * (TB * 16) + l16;
+                __builtin_amdgcn_s_setprio(1);
+                u32x4 raw[2] = {lds_piece(ts, pos0, q4), lds_piece(ts, pos0, q4 + 4)}, wr[WB][2];
+                float sa[TB];
+#pragma unroll
+                for (int i = 0; i < TB; ++i) sa[i] = sa_at[i * 16];
+#pragma unroll
+                for (int b = 0; b < WB; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) wr[b][h] = lds_piece(ws, (wn * WB + b) * 16 + l16, q4 + 4 * h);
+                __builtin_amdgcn_sched_barrier(0);
+                f16x8 wf[WB][4], tf[2];
+                f32x4 r[2][WB];
+#pragma unroll
+                for (int b = 0; b < WB; ++b) wf[b][0] = widen8(wr[b][0][0], wr[b][0][1]);
+                tf[0] = widen8(raw[0][0], raw[0][1]);
+                f16x2 part[4];
+                float f0 = 0.0f, f1 = 0.0f;
+#pragma unroll
+                for (int n = 0; n < TB; ++n) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int h = ((k + 1) & 3) >> 1, u = ((k + 1) & 1) * 2;
+#pragma unroll
+                        for (int b = 0; b < WB; ++b) {
+                            r[n & 1][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wf[b][k], tf[k & 1], k ? r[n & 1][b] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                            if (n + 1 < TB || k < 3)
+#pragma unroll
+                                for (int c = b * 4 / WB; c < (b + 1) * 4 / WB; ++c) part[c] = widen2(raw[h][u + (c >> 1)], c & 1);
+                            if (n == 0 && k < 3) wf[b][k + 1] = widen8(wr[b][h][u], wr[b][h][u + 1]);
+                            if (n > 0) acc[b][n - 1][k] = fmaf(r[n + 1 & 1][b][k], DUAL && b >= HB ? f1 : f0, acc[b][n - 1][k]);
+                            // (waits for LDS count to none: the next read is issued right behind the first use of the one before)
+                            if (b == 0 && (k & 1) && n + 1 < TB) raw[k >> 1] = lds_piece(ts, pos0 + (n + 1) * 16, q4 + 4 * (k >> 1));
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                        if (SPREAD) load_part(n * 4 + k);
+                        tf[k + 1 & 1] = f16x8{part[0][0], part[0][1], part[1][0], part[1][1], part[2][0], part[2][1], part[3][0], part[3][1]};
+                    }
+                    if (n == 0) __builtin_amdgcn_s_setprio(0);
+                    f0 = sa[n] * sw0;
+                    f1 = sa[n] * sw1;
+                }
+#pragma unroll
+                for (int b = 0; b < WB; ++b)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[b][TB - 1][v] = fmaf(r[TB + 1 & 1][b][v], DUAL && b >= HB ? f1 : f0, acc[b][TB - 1][v]);
+            } else {
             Operand<WIDE> wf[WB];
 #pragma unroll
                 for (int b = 0; b < WB; ++b) wf[b].set(lds_operand(ws, (wn * WB + b) * 16 + l16, q4));
@@ -410,14 +485,15 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
                         if (n / WB + 1 < PART) raw = lds_operand(ts, pos0 + (n / WB + 1) * 16, q4);
                     }
                     block_products(wf[n % WB], wf[n % WB + 1], tf, r[n >> 1 & 1][0], r[n >> 1 & 1][1]);
+                    if (SPREAD) load_part(n >> 1);
                     if (n > 0) {
                         add(n - 2);
                         add(n - 1);
                     }
-                    if (WIDE && BM > 64) __builtin_amdgcn_sched_barrier(0);      // hoisted further, reads and widening cost 4 to 7 %
-                }
+                        }
                 add(PART * WB - 2);
                 add(PART * WB - 1);
+            }
             }
             advance(w_read, SW);
             advance(t_read, ST);
@@ -484,7 +560,10 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
                                                                 quotient(acc[b][i][2], s, inv), quotient(acc[b][i][3], s, inv));
             }
         }
-        if (!more) return;
+        if (!more) {
+            if (SPREAD) BM_WAIT_OWN(0)                        // no load may land in LDS that is another's by then
+            return;
+        }
         cur = next;
         lid += share.step;
         buf ^= 1;

@@ -19,15 +19,12 @@ typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// Eight e4m3 values as fp16 (exact: three mantissa bits, exponents down to 2^-9)
+// Two e4m3 values, of the lower or the upper 16 bits, as fp16 (exact: three mantissa bits, exponents down to 2^-9)
 __device__ __forceinline__ f16x2 widen2(uint32_t a, bool high) {
     return high ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
 }
-__device__ __forceinline__ f16x8 widen8(int a, int b) {
-    const f16x2 p = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
-    const f16x2 r = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), s = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
-    return f16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
-}
+__device__ __forceinline__ f16x8 join8(f16x2 p, f16x2 q, f16x2 r, f16x2 s) { return f16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]}; }
+__device__ __forceinline__ f16x8 widen8(uint32_t a, uint32_t b) { return join8(widen2(a, false), widen2(a, true), widen2(b, false), widen2(b, true)); }
 
 // A lane's 32 values of a block of 128: as they are, or as fp16
 template <bool WIDE> struct Operand;
@@ -164,21 +161,20 @@ __device__ __forceinline__ int source_row(const ProductParams &p, int row, int r
     return p.row_map ? row_of_id(p, ldg_i32(p.row_map + pos)) : min(pos, p.a_rows - 1);
 }
 
-// A lane's 32 values of row pos of a stage: pieces q4 and q4 + 4 (any order serves, the same for both operands)
+// Sixteen values of row pos of a stage
 __device__ __forceinline__ u32x4 lds_piece(const uint8_t *rows, int pos, int piece) {
     return *reinterpret_cast<const u32x4 *>(rows + pos * 128 + ((piece ^ ((pos >> 1) & 7)) * 16));
 }
+// A lane's 32 values of row pos of a stage: pieces q4 and q4 + 4 (any order serves, the same for both operands)
 __device__ __forceinline__ i32x8 lds_operand(const uint8_t *rows, int pos, int q4) {
-    const int x = (pos >> 1) & 7;
-    const u32x4 lo = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + ((q4 ^ x) * 16));
-    const u32x4 hi = *reinterpret_cast<const u32x4 *>(rows + pos * 128 + (((q4 + 4) ^ x) * 16));
+    const u32x4 lo = lds_piece(rows, pos, q4), hi = lds_piece(rows, pos, q4 + 4);
     return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
 }
 
 // The block of 128 at which a streaming tile's walk along the reduction begins (it goes round).  Workgroups that start together
 // would otherwise read the same offset of their rows at the same time, which lie a power of two apart in many layers, and
-// meet in few memory channels (5 % of the gate/up product of one token).  A function of the group and the columns: a row's sum does
-// not depend on the rest of the batch.
+// meet in few memory channels (5 % of the gate/up product of one token).  A function of the group and the columns: in tiles of one
+// shape a row's sum does not depend on the rows beside it.
 __device__ __forceinline__ int entry_block(const Tile &t, int kb_n) { return (t.group * 7 + t.nt * 5) % kb_n; }
 
 // Four consecutive values of c
@@ -219,6 +215,12 @@ __device__ uint4 zero_piece;             // where pieces of tokens past the row'
 //   free) -> load the tokens of step s + ST - 1 and the weights of step s + SW - 1 -> multiply.
 // NEAR: the reduction is a multiple of 128, at least MIN_STEPS blocks, and a is smaller than 4 GiB: no piece is cut, addresses are
 // 32-bit offsets (which leaves room for tiles of 192 tokens).
+// SPREAD (128 and 192 rows): the loads of a step stand between its matrix instructions.  Issued together they held a wave for 900 of
+// 6300 cycles, since a unit takes 64 bytes a cycle of them.  Past the last tile they fetch the tile's beginning once more.
+// Bounds.  Few rows: the weights' bytes, 4.5 TB/s at 128 rows of 4096 -> 14336 in 8 groups.  Many rows: the matrix units at the
+// clock that their power leaves.  14336 -> 4096 of 8192 rows: 537 us, 1.79 PFLOP/s (a library's product of 8192^3 in e4m3: 2.7).
+// With e4m3 widened, 4096 -> 14336 of 8192 rows: 1695 us, 1.14 PFLOP/s (in fp16: 1.59), the clock at 2.17 of 2.4 GHz; tiles of 128
+// rows with instructions of 32 x 32 took 3 % fewer cycles, at 1.93 GHz.
 // Everything lies in one LDS array: of several, the compiler tells apart which one direct loads fill, and holds every read
 // of that one until no load is in flight.
 // ---------------------------------------------------------------------------------------------------------------------
@@ -408,9 +410,10 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
                 continue;
             }
             if constexpr (WIDE && BM > 64) {
-                // Beside every matrix instruction stand the widening of the next 32 values of the tokens (in the first 16 tokens, of
-                // the weights too) and the addition of one result of the 16 tokens before: a unit takes a matrix instruction in 16
-                // cycles and the others of the same wave meanwhile
+                // Beside every matrix instruction stand the widening of the next values of the tokens (in the first 16 tokens, of the
+                // weights too) and the addition of one result of the 16 tokens before: a unit works at a matrix instruction for 16
+                // cycles and takes two others of the same wave meanwhile, not three (20.6).  A wave goes first until its first 16
+                // tokens are done, so that the two waves of a unit drift apart (2 %)
                 const int pos0 = wm * (TB * 16) + l16;
                 __builtin_amdgcn_s_setprio(1);
                 u32x4 raw[2] = {lds_piece(ts, pos0, q4), lds_piece(ts, pos0, q4 + 4)}, wr[WB][2];
@@ -441,13 +444,13 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
 #pragma unroll
                                 for (int c = b * 4 / WB; c < (b + 1) * 4 / WB; ++c) part[c] = widen2(raw[h][u + (c >> 1)], c & 1);
                             if (n == 0 && k < 3) wf[b][k + 1] = widen8(wr[b][h][u], wr[b][h][u + 1]);
-                            if (n > 0) acc[b][n - 1][k] = fmaf(r[n + 1 & 1][b][k], DUAL && b >= HB ? f1 : f0, acc[b][n - 1][k]);
+                            if (n > 0) acc[b][n - 1][k] = fmaf(r[(n + 1) & 1][b][k], DUAL && b >= HB ? f1 : f0, acc[b][n - 1][k]);
                             // (waits for LDS count to none: the next read is issued right behind the first use of the one before)
                             if (b == 0 && (k & 1) && n + 1 < TB) raw[k >> 1] = lds_piece(ts, pos0 + (n + 1) * 16, q4 + 4 * (k >> 1));
                             __builtin_amdgcn_sched_barrier(0);
                         }
                         if (SPREAD) load_part(n * 4 + k);
-                        tf[k + 1 & 1] = f16x8{part[0][0], part[0][1], part[1][0], part[1][1], part[2][0], part[2][1], part[3][0], part[3][1]};
+                        tf[(k + 1) & 1] = join8(part[0], part[1], part[2], part[3]);
                     }
                     if (n == 0) __builtin_amdgcn_s_setprio(0);
                     f0 = sa[n] * sw0;
@@ -456,44 +459,44 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
 #pragma unroll
                 for (int b = 0; b < WB; ++b)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[b][TB - 1][v] = fmaf(r[TB + 1 & 1][b][v], DUAL && b >= HB ? f1 : f0, acc[b][TB - 1][v]);
+                    for (int v = 0; v < 4; ++v) acc[b][TB - 1][v] = fmaf(r[(TB + 1) & 1][b][v], DUAL && b >= HB ? f1 : f0, acc[b][TB - 1][v]);
             } else {
-            Operand<WIDE> wf[WB];
+                Operand<WIDE> wf[WB];
 #pragma unroll
                 for (int b = 0; b < WB; ++b) wf[b].set(lds_operand(ws, (wn * WB + b) * 16 + l16, q4));
 #pragma unroll
-            for (int i0 = 0; i0 < TB; i0 += PART) {
-                if (BM <= 64 && live <= i0 * 16) break;              // (in large tiles the branch costs 60 spilled registers)
-                // operands of the next 16 tokens are read, and the results of the block before are added, under the matrix
-                // instructions of the present one
-                const int pos0 = wm * (TB * 16) + i0 * 16 + l16;
-                i32x8 raw = lds_operand(ts, pos0, q4);
-                float sa[PART];
+                for (int i0 = 0; i0 < TB; i0 += PART) {
+                    if (BM <= 64 && live <= i0 * 16) break;              // (in large tiles the branch costs 60 spilled registers)
+                    // operands of the next 16 tokens are read, and the results of the block before are added, under the matrix
+                    // instructions of the present one
+                    const int pos0 = wm * (TB * 16) + i0 * 16 + l16;
+                    i32x8 raw = lds_operand(ts, pos0, q4);
+                    float sa[PART];
 #pragma unroll
-                for (int i = 0; i < PART; ++i) sa[i] = sa_at[(i0 + i) * 16];
-                f32x4 r[2][2];
-                Operand<WIDE> tf;
-                auto add = [&](int n) {
-                    const float f = sa[n / WB] * (DUAL && n % WB >= HB ? sw1 : sw0);
+                    for (int i = 0; i < PART; ++i) sa[i] = sa_at[(i0 + i) * 16];
+                    f32x4 r[2][2];
+                    Operand<WIDE> tf;
+                    auto add = [&](int n) {
+                        const float f = sa[n / WB] * (DUAL && n % WB >= HB ? sw1 : sw0);
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[n % WB][i0 + n / WB][v] = fmaf(r[n >> 1 & 1][n & 1][v], f, acc[n % WB][i0 + n / WB][v]);
-                };
+                        for (int v = 0; v < 4; ++v) acc[n % WB][i0 + n / WB][v] = fmaf(r[n >> 1 & 1][n & 1][v], f, acc[n % WB][i0 + n / WB][v]);
+                    };
 #pragma unroll
-                for (int n = 0; n < PART * WB; n += 2) {
-                    if (n % WB == 0) {
-                        tf.set(raw);
-                        if (n / WB + 1 < PART) raw = lds_operand(ts, pos0 + (n / WB + 1) * 16, q4);
-                    }
-                    block_products(wf[n % WB], wf[n % WB + 1], tf, r[n >> 1 & 1][0], r[n >> 1 & 1][1]);
-                    if (SPREAD) load_part(n >> 1);
-                    if (n > 0) {
-                        add(n - 2);
-                        add(n - 1);
-                    }
+                    for (int n = 0; n < PART * WB; n += 2) {
+                        if (n % WB == 0) {
+                            tf.set(raw);
+                            if (n / WB + 1 < PART) raw = lds_operand(ts, pos0 + (n / WB + 1) * 16, q4);
                         }
-                add(PART * WB - 2);
-                add(PART * WB - 1);
-            }
+                        block_products(wf[n % WB], wf[n % WB + 1], tf, r[n >> 1 & 1][0], r[n >> 1 & 1][1]);
+                        if (SPREAD) load_part(n >> 1);
+                        if (n > 0) {
+                            add(n - 2);
+                            add(n - 1);
+                        }
+                            }
+                    add(PART * WB - 2);
+                    add(PART * WB - 1);
+                }
             }
             advance(w_read, SW);
             advance(t_read, ST);
@@ -572,23 +575,25 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
 
 // ---------------------------------------------------------------------------------------------------------------------
 // One product of few rows a group: the weights' bytes are what counts.  Every wave streams 32 weight rows through a ring of its
-// own in LDS - whole cache lines, no barrier in the loop - WR waves along the weight rows, WK along the reduction (wave k
-// takes every WK-th block of 128, so that the workgroup reads consecutive lines; the parts are added in order at the end).
+// own in LDS - whole cache lines, no barrier in the loop; wave k takes every fourth block of 128, so that the workgroup reads
+// consecutive lines, and the parts are added in order at the end.
 // Tokens go straight to registers, as far ahead as the weights: loads return in order, and waiting for a nearer one would
 // wait for all weights in flight.  Their scales lie in LDS from the start (from memory in the loop they cost as many bytes
-// from the L2 as the tokens: a line for four).
+// from the L2 as the tokens: a line for four).  Measured at 1 row, 4096 -> 4096: 9.4 us, of which 5 are the launch and the first
+// and last bytes' way; 14336 -> 4096, two groups of one row: 21.7 us, 5.4 TB/s.
 // ---------------------------------------------------------------------------------------------------------------------
+constexpr int STREAM_WAVES = 4;
 constexpr int STREAM_SCALES = 32 * 112;          // tokens x blocks of 128 whose scales fit beside the ring
 
-template <int TB, int WR, int WK, int S, bool WIDE>
+template <int TB, bool WIDE>
 __device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &t, int rows, uint8_t *ring, const float *s_sw, const float *s_sa,
                                             const uint8_t *b0) {
-    constexpr int WB = 2, PER = 4 + 2 * TB;
+    constexpr int WB = 2, S = 4, PER = 4 + 2 * TB;              // stages; loads of a step
     static_assert((S - 2) * PER < 64, "the wait counts up to 63 loads");
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int wr = wave % WR, wk = wave / WR, q4 = lane >> 4, l16 = lane & 15;
+    const int q4 = lane >> 4, l16 = lane & 15;
     const int N = p.N, Kd = p.Kd, kb_n = (Kd + SCALE_BLOCK - 1) / SCALE_BLOCK;
-    const int row0 = t.row0, row_end = t.row_end, n0 = t.nt * (32 * WR);
+    const int row0 = t.row0, row_end = row0 + rows, n0 = t.nt * 32;      // the tile's rows, fewer than the matrix instruction's
     uint8_t *mine = ring + wave * (S * 4096);
 
     const uint8_t *wp[4];
@@ -596,7 +601,7 @@ __device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int pos = j * 8 + (lane >> 3), b = pos >> 4, m = pos & 15;
-        const int n = min(n0 + wr * 32 + (m >> 2) * 8 + b * 4 + (m & 3), N - 1);         // a lane's results: consecutive columns
+        const int n = min(n0 + (m >> 2) * 8 + b * 4 + (m & 3), N - 1);         // a lane's results: consecutive columns
         wp[j] = b0 + (size_t)n * Kd + ((piece ^ (4 * (j & 1))) * 16);
     }
     const uint8_t *tp[TB];
@@ -609,9 +614,9 @@ __device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &
 #pragma unroll
         for (int i = 0; i < TB; ++i) acc[b][i] = 0.0f;
 
-    const int steps = (kb_n - wk + WK - 1) / WK, entry = entry_block(t, kb_n);
+    const int steps = (kb_n - wave + STREAM_WAVES - 1) / STREAM_WAVES, entry = entry_block(t, kb_n);
     auto block_of = [&](int step) {
-        const int kt = wk + min(step, steps - 1) * WK + entry;      // past the end: the last one again
+        const int kt = wave + min(step, steps - 1) * STREAM_WAVES + entry;      // past the end: the last one again
         return kt < kb_n ? kt : kt - kb_n;
     };
     auto issue = [&](int step, int st, u32x4 (&lo)[TB], u32x4 (&hi)[TB]) {
@@ -671,32 +676,25 @@ __device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &
     BM_WAIT_OWN(0)                                                     // nothing may land in LDS that others use, or behind the end
     constexpr int PAIRS = WB * TB;
     auto put = [&](int b, int i, f32x4 v) {
-        const int col = n0 + wr * 32 + q4 * 8 + b * 4, r = row0 + i * 16 + l16;
+        const int col = n0 + q4 * 8 + b * 4, r = row0 + i * 16 + l16;
         if (col < N && r < row_end) store4(p, (size_t)r * N + col, v);
     };
-    if (WK == 1) {
-#pragma unroll
-        for (int pair = 0; pair < PAIRS; ++pair) put(pair / TB, pair % TB, acc[pair / TB][pair % TB]);
-        return;
-    }
     __syncthreads();                                                   // every ring is done with: the parts take its place
     float *red = reinterpret_cast<float *>(ring);                      // [wave][pair of blocks][lane], four at a time
 #pragma unroll
     for (int pair = 0; pair < PAIRS; ++pair) *reinterpret_cast<f32x4 *>(red + ((wave * PAIRS + pair) * 64 + lane) * 4) = acc[pair / TB][pair % TB];
     __syncthreads();
-    for (int pair = wk; pair < PAIRS; pair += WK) {
+    for (int pair = wave; pair < PAIRS; pair += STREAM_WAVES) {
         f32x4 sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < WK; ++k) sum += *reinterpret_cast<const f32x4 *>(red + (((k * WR + wr) * PAIRS + pair) * 64 + lane) * 4);
+        for (int k = 0; k < STREAM_WAVES; ++k) sum += *reinterpret_cast<const f32x4 *>(red + ((k * PAIRS + pair) * 64 + lane) * 4);
         put(pair / TB, pair % TB, sum);
     }
 }
 
-template <int WR, int WK, bool WIDE>
-__global__ void __launch_bounds__(WR * WK * 64, 2) stream_kernel(ProductParams p, int bm) {
-    constexpr int COLS = 32 * WR;
-    static_assert(SCALE_BLOCK % COLS == 0, "a tile's columns: one block of scales");
-    constexpr int RING = WR * WK * 4 * 4096, MAX_KB = MAX_PRODUCT_KD / SCALE_BLOCK;
+template <bool WIDE>
+__global__ void __launch_bounds__(STREAM_WAVES * WAVE, 2) stream_kernel(ProductParams p, int bm) {
+    constexpr int COLS = 32, RING = STREAM_WAVES * 4 * 4096, MAX_KB = MAX_PRODUCT_KD / SCALE_BLOCK;
     __shared__ __attribute__((aligned(1024))) uint8_t ring[RING + (MAX_KB + STREAM_SCALES) * 4];
     float *const s_sw = reinterpret_cast<float *>(ring + RING), *const s_sa = s_sw + MAX_KB;
     TileTable &tt = *reinterpret_cast<TileTable *>(ring);                   // gone when the ring is filled
@@ -708,14 +706,14 @@ __global__ void __launch_bounds__(WR * WK * 64, 2) stream_kernel(ProductParams p
     const Tile t = tile_at(p, tt, bm, n_nt, share.begin);
     const Matrices m = matrices_of<false>(p, t.group);
     const int rows = min(t.row_end - t.row0, bm), kb_n = (p.Kd + SCALE_BLOCK - 1) / SCALE_BLOCK;
-    for (int kb = threadIdx.x; kb < kb_n; kb += WR * WK * 64) s_sw[kb] = ldg_f32(m.s0 + (size_t)(t.nt * COLS / SCALE_BLOCK) * kb_n + kb);
-    for (int r = threadIdx.x >> 6; r < rows; r += WR * WK) {
+    for (int kb = threadIdx.x; kb < kb_n; kb += STREAM_WAVES * WAVE) s_sw[kb] = ldg_f32(m.s0 + (size_t)(t.nt * COLS / SCALE_BLOCK) * kb_n + kb);
+    for (int r = threadIdx.x >> 6; r < rows; r += STREAM_WAVES) {
         const float *src = p.a_scale + (size_t)source_row(p, t.row0 + r, t.row_end) * kb_n;
         for (int k = threadIdx.x & 63; k < kb_n; k += 64) s_sa[r * kb_n + k] = ldg_f32(src + k);
     }
     __syncthreads();
-    if (rows <= 16) stream_tile<1, WR, WK, 4, WIDE>(p, t, rows, ring, s_sw, s_sa, m.w0);
-    else stream_tile<2, WR, WK, 4, WIDE>(p, t, rows, ring, s_sw, s_sa, m.w0);
+    if (rows <= 16) stream_tile<1, WIDE>(p, t, rows, ring, s_sw, s_sa, m.w0);
+    else stream_tile<2, WIDE>(p, t, rows, ring, s_sw, s_sa, m.w0);
 }
 
 // A bound on the row tiles of any grouping of the rows, times the column tiles.
@@ -742,12 +740,21 @@ template <bool WIDE>
 static void launch_stream(const ProductParams &p, hipStream_t st) {
     const int kb_n = (p.Kd + SCALE_BLOCK - 1) / SCALE_BLOCK, bm = 32 * kb_n <= STREAM_SCALES ? 32 : 8;
     const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, bm, 32) + 7) / 8 * 8;
-    hipLaunchKernelGGL((stream_kernel<1, 4, WIDE>), dim3((unsigned)tiles), dim3(256), 0, st, p, bm);
+    hipLaunchKernelGGL((stream_kernel<WIDE>), dim3((unsigned)tiles), dim3(STREAM_WAVES * WAVE), 0, st, p, bm);
 }
 
+// Tiles by the rows a group has on average (groups of experts that are not resident are empty: the live ones have more).  A
+// larger tile reads its operands fewer times and computes on more rows that are none; with fewer than a tile for each of the 256
+// units the smaller one wins.  Measured in us, 14336 -> 4096 of 8 groups, rows a group and tiles of 192 | 128 | 64 | 32 rows:
+//   256: 211 251 273 369    128: 203 149 183 221    64: 304 145 158 161    32: 278 145 110 119    8: 174 114 88 68
+// and 768 -> 2048 of 128 groups:
+//   512: 208 240 298 433     64: 55 46 53 72        32: 46 36 35 43        16: 50 35 31 34        4: 33 21 20 19
+// Tiles of 32 rows: at 2048 -> .. and beyond the reduction is worth two parts within a workgroup (14336 -> 4096 of 16 rows: 56 us
+// against 69; of 512 rows, 768 -> 2048: 59 against 43).  Up to 128 tiles the streaming kernel takes 9.4 us for 1 x 4096 x 4096 against
+// 17, 18.5 for 64 x 1024 x 8192 against 34; with more it is even (58.6 against 60 for 16 rows of 14336 -> 4096 in 8 groups).
 template <bool WIDE>
 static void launch_product_t(const ProductParams &p, hipStream_t st) {
-    const long long avg = p.rows / p.n_groups;                // (groups of experts that are not resident are empty: the live ones have more)
+    const long long avg = p.rows / p.n_groups;
     auto tiles = [&](int bm, int bn) { return tiles_bound(p.rows, p.N, p.n_groups, bm, bn); };
     if (avg >= 256 && tiles(192, 256) >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, false, WIDE>(p, st);
     else if (avg >= 48 && tiles(128, 128) >= 256) launch_tiles<128, 128, 2, 4, 1, 2, 2, 2, false, WIDE>(p, st);
@@ -763,10 +770,15 @@ int launch_product(const ProductParams &p, hipStream_t st) {
     return launch_status(__func__);
 }
 
+// As above, with 128 columns of both matrices a tile.  Measured in us, gate/up 4096 -> 14336 of 8 groups, rows a group and tiles
+// of 192 | 128 | 32 rows:   1024: 1695 . .    256: 534 549 731    128: 324 330 416    64: . 218 240    16: 186 169 130
+// and 2048 -> 768 of 128 groups:   512: 472 490 670    128: . 153 198    64: . 110 104    32: 104 80 69
+// Tiles of 32 rows, up to two for each unit: four stages and one workgroup a unit, else two and two (two rows, 4096 -> 14336: 41 us
+// against 49; 128 rows of it in 8 groups: 138 against 130).
 int launch_swiglu(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
     if (avg >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, true, true>(p, st);
-    else if (avg >= 96) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, true, true>(p, st);
+    else if (avg >= (p.Kd >= 4096 ? 64 : 96)) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, true, true>(p, st);
     else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= 512) launch_tiles<32, 256, 1, 8, 1, 4, 4, 1, true, true>(p, st);
     else launch_tiles<32, 256, 1, 8, 1, 2, 2, 2, true, true>(p, st);
     return launch_status(__func__);

@@ -324,11 +324,12 @@ typedef struct {
 /* q [n][rows][cols] and scale [n][rows / block_rows, rounded up][ceil(cols/128)] of
  * src [n][rows][cols] (all device).  Weights are quantized once, at load time; any
  * width is taken, whole 16-byte pieces at a time where cols is a multiple of 8 and the
- * arrays are aligned. */
+ * arrays are aligned; fewer than 2^28 - 16 blocks of rows, or
+ * up to 65535 matrices of 65535 rows of blocks. */
 int bm_quantize(const bm_quantize_desc *desc, const void *src, void *q, float *scale, void *stream);
 
 typedef struct {
-    int32_t T, d;            /* rows and width, 1 <= d <= 16384                              */
+    int32_t T, d;            /* rows and width, 1 <= d <= 16384, T * d / 8 under 2^32        */
     int32_t dtype;           /* of x, residual, gamma, residual_out, y: BM_F32 or BM_BF16    */
     float eps;               /* >= 0, added to the mean square                               */
 } bm_norm_desc;
@@ -358,18 +359,22 @@ typedef struct {
  * w_scale [E][ceil(N/128)][ceil(Kd/128)], c [rows][N] (all device).  r(i) = row_map[i] / K
  * (row_map [rows] device int32: bm_permute_by_expert's perm with the layer's K), or i
  * with row_map NULL (a_rows >= rows then).  offsets [E+1] device int32, or NULL with
- * E = 1: one group of all rows.  Products of a block of 128 are summed by the matrix
- * unit in fp32, blocks are scaled and added in fp32 in order; c is rounded once.  Rows of
- * c behind offsets[E] are left as they were, groups without rows read nothing.  Offsets
- * are taken as clamped to [0, rows] and no smaller than those before them, mapped
- * rows as clamped to [0, a_rows).  Equal calls give equal bits. */
+ * E = 1: one group of all rows.  Sums are fp32: a block's 128 products in the matrix
+ * unit, then the blocks, scaled, one after the other, from a block and in up to four
+ * parts that depend on the sizes; c is rounded once.  The two scales of a block are
+ * multiplied first: their product has to lie within fp32's normal range.  With c in bf16
+ * the matrix unit may cut each of the eight products that it adds at once below 2^-13 of
+ * the largest (1.4e-5 of a result's 2-norm, far under its rounding).  Rows of c behind
+ * offsets[E] are left as they were, groups without rows read nothing.  Offsets are taken
+ * as clamped to [0, rows] and no smaller than those before them, mapped rows as clamped
+ * to [0, a_rows).  Equal calls give equal bits. */
 int bm_grouped_matmul(const bm_product_desc *desc, const void *a, const float *a_scale, const int32_t *row_map,
                       const int32_t *offsets, const void *w, const float *w_scale, void *c, void *stream);
 
 /* Two such products and what an expert does with them:
  *   h[i] = silu(a[r(i)] . w_gate[e]) * (a[r(i)] . w_up[e])          (fp32)
  * written as 8-bit h [rows][N] with h_scale [rows][ceil(N/128)]: the input of
- * bm_grouped_matmul with the down matrices. */
+ * bm_grouped_matmul with the down matrices.  The sums are those of an fp32 c. */
 int bm_grouped_swiglu(const bm_product_desc *desc, const void *a, const float *a_scale, const int32_t *row_map,
                       const int32_t *offsets, const void *w_gate, const float *gate_scale, const void *w_up,
                       const float *up_scale, void *h, float *h_scale, void *stream);

@@ -375,7 +375,10 @@ int stage_events(const bm_debug_out *dbg, hipEvent_t (&ev)[5]) {
 
 // ---- the layer on 8-bit weights -------------------------------------------------------------------------------------
 
-constexpr int O_F32_TOKENS = 256;    // up to this many tokens an expert's output is held in fp32 (it is small, and y one rounding more exact)
+// Up to this many tokens an expert's output is held in fp32: it is small beside the weights, and y one rounding more exact.  Beyond, bf16
+// halves its way to the aggregation and lets the down product multiply 8 bits as they are (8192 rows of 14336 -> 4096: 1.8 PFLOP/s
+// against 1.1 with e4m3 widened).
+constexpr int O_F32_TOKENS = 256;
 
 // Workspace of bm_moe_forward_quantized: the front end's arrays, the 8-bit tokens, h and the experts' outputs.
 struct QuantizedLayout {
@@ -389,7 +392,7 @@ int check_quantized_desc(const bm_layer_desc *d) {
     if (rc) return rc;
     if (d->dtype != BM_BF16) return BM_ERR_DTYPE;
     if (d->d > MAX_PRODUCT_KD || d->F > MAX_PRODUCT_KD) return BM_ERR_SHAPE;
-    if ((long long)d->T * (d->K + d->n_shared) > (1ll << 30)) return BM_ERR_SHAPE;
+    if ((long long)d->T * (d->K + d->n_shared) > (1ll << 30) || !quantize_grid_ok(1, d->T, d->d, false)) return BM_ERR_SHAPE;
     return BM_OK;
 }
 
@@ -801,6 +804,7 @@ int bm_add_rmsnorm(const bm_norm_desc *d, const void *x, const void *residual, c
     if (!d) return BM_ERR_NULL;
     if (d->dtype != BM_F32 && d->dtype != BM_BF16) return BM_ERR_DTYPE;
     if (d->T < 0 || d->d <= 0 || d->d > MAX_NORM_D || !(d->eps >= 0.0f) || d->eps > 3.0e38f) return BM_ERR_SHAPE;
+    if (!norm_grid_ok(d->T, d->d)) return BM_ERR_SHAPE;
     if (d->T == 0) return BM_OK;
     if (!x || !gamma || (q && !scale) || (!residual_out && !y && !q)) return BM_ERR_NULL;
     if (y && y == residual_out) return BM_ERR_SHAPE;

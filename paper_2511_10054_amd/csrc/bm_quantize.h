@@ -40,8 +40,15 @@ struct NormParams {
 // the launch's grid stays within its limits
 inline bool quantize_grid_ok(int n, int rows, int cols, bool blocks) {
     const long long kb = ((long long)cols + SCALE_BLOCK - 1) / SCALE_BLOCK, rb = ((long long)rows + SCALE_BLOCK - 1) / SCALE_BLOCK;
-    return blocks ? rb <= 65535 && n <= 65535 : (long long)n * rows < (1ll << 40) / kb && ((long long)n * rows * kb + 15) / 16 < (1ll << 31);
+    return blocks ? rb <= 65535 && n <= 65535 : (long long)n * rows <= ((1ll << 28) - 16) / kb;      // 16 threads a block, under 2^32 a launch
 }
+
+// Threads of a norm's workgroup: eight values each, in whole waves, twice eight past 8192
+inline int norm_threads(int d) {
+    const int nt = ((d + 7) / 8 + 63) / 64 * 64;
+    return nt < 1024 ? nt : 1024;
+}
+inline bool norm_grid_ok(int T, int d) { return (long long)T * norm_threads(d) < (1ll << 32); }
 
 int launch_add_rmsnorm(const NormParams &p, bool f32, hipStream_t st);
 int launch_quantize(const void *src, bool f32, uint8_t *q, float *scale, int n, int rows, int cols, bool blocks, hipStream_t st);

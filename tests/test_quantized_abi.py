@@ -38,7 +38,7 @@ def test_status_of_misaligned_arrays_has_a_text():
 @pytest.mark.parametrize("over,args,want", [
     (dict(), (ONE, ONE, None), NULL), (dict(), (None, ONE, ONE), NULL), (dict(), (ONE, None, ONE), NULL),
     (dict(dtype=7), (ONE, ONE, ONE), DTYPE), (dict(block_rows=64), (ONE, ONE, ONE), SHAPE), (dict(rows=-1), (ONE, ONE, ONE), SHAPE),
-    (dict(n=70000, block_rows=128), (ONE, ONE, ONE), SHAPE), (dict(n=1 << 20, rows=1 << 20, cols=1 << 20), (ONE, ONE, ONE), SHAPE),
+    (dict(n=70000, block_rows=128), (ONE, ONE, ONE), SHAPE), (dict(n=1 << 20, rows=1 << 20, cols=1 << 20), (ONE, ONE, ONE), SHAPE), (dict(n=1 << 14, rows=1 << 14, cols=1), (ONE, ONE, ONE), SHAPE),
     (dict(rows=0), (None, None, None), 0), (dict(cols=0), (None, None, None), 0), (dict(n=0), (None, None, None), 0),
 ])
 def test_quantize_refusals(over, args, want):
@@ -55,7 +55,7 @@ def test_quantize_refusals(over, args, want):
     (dict(d=0), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE), (dict(T=-1), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE),
     (dict(eps=-1.0), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE), (dict(eps=float("nan")), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE),
     (dict(eps=float("inf")), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE), (dict(dtype=3), (ONE,) * 4 + (ODD, ONE, ONE), DTYPE),
-    (dict(T=0), (None,) * 7, 0),
+    (dict(T=0), (None,) * 7, 0), (dict(T=1 << 22, d=8192), (ONE,) * 4 + (ODD, ONE, ONE), SHAPE),
 ])
 def test_norm_refusals(over, args, want):
     d = bm.NormDesc(**dict(dict(T=4, d=64, dtype=bm.BM_F32, eps=1e-6), **over))

@@ -886,11 +886,18 @@ int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const voi
     FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
                              at<float>(ws, Q.o), (size_t)L.rows_max * desc->d * (Q.o_f32 ? 4 : 2));
     fe.sp.BM = 1 << 30;                       // the products find their tiles from the offsets: the table is not read
+    uint8_t *const own_q = at<uint8_t>(ws, Q.xq);
+    float *const own_s = at<float>(ws, Q.xs);
+    const bool beside = !x_q && front_quantizes(fe.fp, fe.fuse);
+    if (beside) {
+        fe.fp.xq = own_q;
+        fe.fp.xs = own_s;
+    }
     err |= launch_front_end(desc, fe, ws, L, st);
     if (!x_q) {
-        err |= launch_quantize(x, false, at<uint8_t>(ws, Q.xq), at<float>(ws, Q.xs), 1, T, desc->d, false, st);
-        x_q = at<uint8_t>(ws, Q.xq);
-        x_scale = at<float>(ws, Q.xs);
+        if (!beside) err |= launch_quantize(x, false, own_q, own_s, 1, T, desc->d, false, st);
+        x_q = own_q;
+        x_scale = own_s;
     }
     mark(1);
 

@@ -74,6 +74,8 @@ struct FrontParams {
     int tile_tokens;        // tokens per workgroup: TILE_T, or 16 for small batches and fp32 (see front_tile_tokens)
     ScanParams scan;        // used when fused or tail
     ScatterParams scat;     // used when fused or tail
+    uint8_t *xq;            // [T][d]: workgroups behind those of the tiles write x's 8-bit form (front_quantizes), or null
+    float *xs;              // [T][ceil(d / 128)], its scales
 };
 
 
@@ -134,6 +136,7 @@ struct CombineParams {
 // the kernel and the HIP error) otherwise
 int launch_status(const char *what);
 
+bool front_quantizes(const FrontParams &p, bool fused);
 bool front_can_fuse(int T, int dtype, uint32_t flags);   // the batch is small enough for the one-workgroup front end
 int front_tile_tokens(int T, int dtype, bool fused);   // tokens per workgroup of the front kernel
 bool front_wants_logits(const FrontParams &p, int dtype);   // FrontParams::logits pays if there is room for it

@@ -183,6 +183,28 @@ def test_own_8_bit_tokens_are_bm_quantizes():
 
 
 @pytest.mark.parametrize("name,over,T,kw", [
+    ("c4_qwen3", dict(d=256, F=64), 1, dict()), ("c5_deepseek", dict(d=96, F=64), 17, dict()), ("c2_mixtral_decode", dict(d=4096, F=32), 64, dict()),
+    ("c4_qwen3", dict(d=160, F=32, E=256, n_resident=128), 40, dict()), ("c4_qwen3", dict(d=256, F=32), 2800, dict()),      # beside 16 | 8 waves, apart
+    ("c4_qwen3", dict(d=288, F=32), 20, dict(beta=0.4)), ("c5_deepseek", dict(d=288, F=32), 90, dict(beta=0.4)),            # behind the batch's gate
+])
+def test_own_8_bit_tokens_at_every_front_end(name, over, T, kw):
+    """Wherever the tokens' 8-bit form is made, y is what the tokens that bm_quantize makes give, call after call."""
+    print("own tokens", name, over, T, kw, flush=True)
+    L = Quantized(name, over, T, **kw)
+    d = L.spec.d
+    q, s = torch.empty((T, d), dtype=torch.uint8, device="cuda"), torch.empty((T, -(-d // BLOCK)), device="cuda")
+    for turn in range(2):
+        if turn:
+            L.x.copy_(L.x.flip(0).clone() * 1.5)                           # other values in the same buffers
+        L.forward(debug=False)
+        own = L.y.clone()
+        bm.bm_quantize(bm.QuantizeDesc(n=1, rows=T, cols=d, block_rows=1, dtype=bm.BM_BF16), L.x, q, s)
+        L.work.fill_(0xA5)
+        L.forward(q, s, debug=False)
+        assert torch.equal(L.y, own) and torch.isfinite(own.float()).all()
+
+
+@pytest.mark.parametrize("name,over,T,kw", [
     ("c4_qwen3", dict(d=256, F=256), 8, dict()), ("c5_deepseek", dict(d=256, F=352), 40, dict(rho=1)),
     ("c2_mixtral_decode", dict(d=512, F=512), 400, dict()), ("c4_qwen3", dict(d=256, F=128), 40, dict(beta=1.5))])
 def test_replays_equal_eager(name, over, T, kw):

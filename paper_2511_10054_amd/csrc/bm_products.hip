@@ -773,13 +773,15 @@ int launch_product(const ProductParams &p, hipStream_t st) {
 // As above, with 128 columns of both matrices a tile.  Measured in us, gate/up 4096 -> 14336 of 8 groups, rows a group and tiles
 // of 192 | 128 | 32 rows:   1024: 1695 . .    256: 534 549 731    128: 324 330 416    64: . 218 240    16: 186 169 130
 // and 2048 -> 768 of 128 groups:   512: 472 490 670    128: . 153 198    64: . 110 104    32: 104 80 69
-// Tiles of 32 rows, up to two for each unit: four stages and one workgroup a unit, else two and two (two rows, 4096 -> 14336: 41 us
-// against 49; 128 rows of it in 8 groups: 138 against 130).
+// Tiles of 32 rows: four stages and one workgroup a unit, or two and two.  The first wins where tiles are fewer than units (two rows,
+// 4096 -> 14336: 41 us against 49) and in the last round of long reductions, whose tiles have a unit each (4096 -> 8192, 640 tiles: 121
+// against 130, 768: 138 against 139, 1024: 183 against 182); the second where a second round would hold few tiles (2048 -> 768 of 512 rows in
+// 128 groups, half of them empty: 46 against 37) and with more rows a tile (4096 -> 14336 of 128 rows in 8 groups: 137 against 130).
 int launch_swiglu(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
     if (avg >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, true, true>(p, st);
     else if (avg >= (p.Kd >= 4096 ? 64 : 96)) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, true, true>(p, st);
-    else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= 512) launch_tiles<32, 256, 1, 8, 1, 4, 4, 1, true, true>(p, st);
+    else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= (p.Kd >= 4096 ? 1024 : 512)) launch_tiles<32, 256, 1, 8, 1, 4, 4, 1, true, true>(p, st);
     else launch_tiles<32, 256, 1, 8, 1, 2, 2, 2, true, true>(p, st);
     return launch_status(__func__);
 }

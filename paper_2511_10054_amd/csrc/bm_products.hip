@@ -749,6 +749,8 @@ static void launch_stream(const ProductParams &p, hipStream_t st) {
 //   256: 211 251 273 369    128: 203 149 183 221    64: 304 145 158 161    32: 278 145 110 119    8: 174 114 88 68
 // and 768 -> 2048 of 128 groups:
 //   512: 208 240 298 433     64: 55 46 53 72        32: 46 36 35 43        16: 50 35 31 34        4: 33 21 20 19
+// Tiles of 128 rows: 256 columns for long reductions of 8-bit instructions (14336 -> 4096 of 1024 rows in 8 groups: 134 us against 147),
+// else 128 and two workgroups a unit (768 -> 2048 of 8192 rows in 128 groups: 46 against 49; of 512 rows, 14336 -> 4096 in fp32: 149 against 187).
 // Tiles of 32 rows: at 2048 -> .. and beyond the reduction is worth two parts within a workgroup (14336 -> 4096 of 16 rows: 56 us
 // against 69; of 512 rows, 768 -> 2048: 59 against 43).  Up to 128 tiles the streaming kernel takes 9.4 us for 1 x 4096 x 4096 against
 // 17, 18.5 for 64 x 1024 x 8192 against 34; with more it is even (58.6 against 60 for 16 rows of 14336 -> 4096 in 8 groups).
@@ -756,8 +758,11 @@ template <bool WIDE>
 static void launch_product_t(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
     auto tiles = [&](int bm, int bn) { return tiles_bound(p.rows, p.N, p.n_groups, bm, bn); };
+    const bool long_rows = !WIDE && p.Kd >= 4096 && avg >= 128 && tiles(128, 256) >= 256;
     if (avg >= 256 && tiles(192, 256) >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, false, WIDE>(p, st);
-    else if (avg >= 48 && tiles(128, 128) >= 256) launch_tiles<128, 128, 2, 4, 1, 2, 2, 2, false, WIDE>(p, st);
+    else if (long_rows) {
+        if constexpr (!WIDE) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, false, false>(p, st);
+    } else if (avg >= 48 && tiles(128, 128) >= 256) launch_tiles<128, 128, 2, 4, 1, 2, 2, 2, false, WIDE>(p, st);
     else if (avg >= (p.Kd >= 2048 ? 32 : 16) && tiles(64, 128) >= 256) launch_tiles<64, 128, 2, 4, 1, 3, 3, 2, false, WIDE>(p, st);
     else if (p.Kd >= 2048 && tiles(32, 128) <= 128) launch_stream<WIDE>(p, st);
     else if (p.Kd >= 2048) launch_tiles<32, 128, 1, 4, 2, 3, 3, 1, false, WIDE>(p, st);

@@ -64,6 +64,15 @@ __device__ __forceinline__ void block_products(const Operand<true> &a0, const Op
 }
 
 #define BM_LDS __attribute__((address_space(3)))
+// BYTES of every lane from base + offset + step into LDS, in the order of the lanes; offset + step + BYTES stay below 2^32 - 1, where the
+// buffer ends.  A buffer instruction: behind a global one that writes LDS the compiler holds every use of an LDS read until all
+// reads before it are done (2 to 4 % of the large products).
+template <int BYTES>
+__device__ __forceinline__ void fetch(const void *base, uint32_t offset, uint32_t step, void *lds) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, -1, 0x00027000);
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BM_LDS void *)lds, 16, (int)offset, (int)step, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (BM_LDS void *)lds, 4, (int)offset, (int)step, 0, 0);
+}
 // At most n direct loads of this wave are still in flight and its LDS accesses are done; then all waves meet.
 // (s_waitcnt of gfx9: vmcnt[3:0] | expcnt 7 << 4 | lgkmcnt 0 << 8 | vmcnt[5:4] << 14)
 #define BM_WAIT_AND_MEET(n)                                                             \
@@ -307,24 +316,28 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
     auto load_weight = [&](int step, int slot, int j) {
         const int kt = block_at(step, w_entry), k0 = NEAR || kt < kb_n ? kt * 128 : 0;
         const int pos = wave * (WI * 8) + j * 8, pc = w_piece(j) * 16;
-        const uint8_t *from = (DUAL && (pos >> 4) % WB >= HB ? wt.w1 : wt.w0) + k0;
+        const uint8_t *from = DUAL && (pos >> 4) % WB >= HB ? wt.w1 : wt.w0;
         const uint32_t off = NEAR || k0 + pc < Kd ? wo[j] : wo[j] - pc;
-        __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(from + off), (BM_LDS void *)(w_ring + (slot * KG + kg) * (BN * 128) + pos * 128), 16, 0, 0);
+        fetch<16>(from, off, k0, w_ring + (slot * KG + kg) * (BN * 128) + pos * 128);
     };
     auto load_token = [&](int step, int slot, int j) {
         const int kt = block_at(step, t_entry), k0 = kt * 128;
         if (j < TI) {
-            const uint8_t *src;
-            if constexpr (NEAR) src = p.a + k0 + to[j];
-            else src = k0 + t_piece(j) * 16 < Kd ? tp[j] + k0 : reinterpret_cast<const uint8_t *>(&zero_piece);
-            if (TR >= 8 || lane < TR * 8)
-                __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)(t_ring + (slot * KG + kg) * (BM * 128) + (wave * TR + j * 8) * 128), 16, 0, 0);
+            uint8_t *lds_at = t_ring + (slot * KG + kg) * (BM * 128) + (wave * TR + j * 8) * 128;
+            if (TR >= 8 || lane < TR * 8) {
+                if constexpr (NEAR) {
+                    fetch<16>(p.a, to[j], k0, lds_at);
+                } else {
+                    const uint8_t *src = k0 + t_piece(j) * 16 < Kd ? tp[j] + k0 : reinterpret_cast<const uint8_t *>(&zero_piece);
+                    __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)src, (BM_LDS void *)lds_at, 16, 0, 0);
+                }
+            }
         } else {
-            const float *sc;
-            if constexpr (NEAR) sc = p.a_scale + kt + so;
-            else sc = sp + min(kt, kb_n - 1);
-            if (lane < TR)
-                __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)sc, (BM_LDS void *)(s_sa + (slot * KG + kg) * BM + wave * TR), 4, 0, 0);
+            float *lds_at = s_sa + (slot * KG + kg) * BM + wave * TR;
+            if (lane < TR) {
+                if constexpr (NEAR) fetch<4>(p.a_scale, so * 4, kt * 4, lds_at);
+                else __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(sp + min(kt, kb_n - 1)), (BM_LDS void *)lds_at, 4, 0, 0);
+            }
         }
     };
     auto load_weights = [&](int step, int slot) {
@@ -341,10 +354,9 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
         const Matrices m = matrices_of<DUAL>(p, t.group);
         const float *s = (DUAL && j ? m.s1 : m.s0) + (size_t)nb * kb_n;
         if (j < 2 && kb < kb_n)
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(s + kb), (BM_LDS void *)(s_sw + (buf * 2 + j) * MAX_KB + (all & 3) * 64), 4, 0, 0);
+            fetch<4>(s, kb * 4, 0, s_sw + (buf * 2 + j) * MAX_KB + (all & 3) * 64);
         if (ids && p.row_map && lane < TR)
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(p.row_map + min(t.row0 + wave * TR + lane, t.row_end - 1)),
-                                             (BM_LDS void *)(s_id + wave * TR), 4, 0, 0);
+            fetch<4>(p.row_map + t.row0, (uint32_t)min(wave * TR + lane, t.row_end - 1 - t.row0) * 4, 0, s_id + wave * TR);
     };
 
     int lid = share.begin;
@@ -421,9 +433,9 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
 #pragma unroll
                 for (int i = 0; i < TB; ++i) sa[i] = sa_at[i * 16];
 #pragma unroll
-                for (int b = 0; b < WB; ++b)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) wr[b][h] = lds_piece(ws, (wn * WB + b) * 16 + l16, q4 + 4 * h);
+                    for (int b = 0; b < WB; ++b) wr[b][h] = lds_piece(ws, (wn * WB + b) * 16 + l16, q4 + 4 * h);
                 __builtin_amdgcn_sched_barrier(0);
                 f16x8 wf[WB][4], tf[2];
                 f32x4 r[2][WB];
@@ -445,7 +457,6 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
                                 for (int c = b * 4 / WB; c < (b + 1) * 4 / WB; ++c) part[c] = widen2(raw[h][u + (c >> 1)], c & 1);
                             if (n == 0 && k < 3) wf[b][k + 1] = widen8(wr[b][h][u], wr[b][h][u + 1]);
                             if (n > 0) acc[b][n - 1][k] = fmaf(r[(n + 1) & 1][b][k], DUAL && b >= HB ? f1 : f0, acc[b][n - 1][k]);
-                            // (waits for LDS count to none: the next read is issued right behind the first use of the one before)
                             if (b == 0 && (k & 1) && n + 1 < TB) raw[k >> 1] = lds_piece(ts, pos0 + (n + 1) * 16, q4 + 4 * (k >> 1));
                             __builtin_amdgcn_sched_barrier(0);
                         }

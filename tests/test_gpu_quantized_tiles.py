@@ -146,10 +146,11 @@ def test_swiglu_in_every_tile_shape(counts, N, Kd, K):
 # ---- offsets past 32 bits ----------------------------------------------------------------------------------------------
 
 
-@pytest.mark.parametrize("rows", [40, 600])
-def test_gathered_rows_past_4_gib(rows):
-    print("rows past 4 GiB", rows, flush=True)
-    N, Kd, a_rows = 1056, 4096, 1_100_000
+@pytest.mark.parametrize("rows", [40, 600, 2000])
+@pytest.mark.parametrize("a_rows", [(1 << 20) - 1, 1_100_000])             # the last row short of 4 GiB (32-bit offsets) and past it
+def test_gathered_rows_around_4_gib(rows, a_rows):
+    print("rows around 4 GiB", rows, a_rows, flush=True)
+    N, Kd = 1056 if rows < 2000 else 6272, 4096                            # (tiles of 192 rows for the most)
     o = Operands([rows], N, Kd, rows)
     a, sa = torch.empty((a_rows, Kd), dtype=torch.uint8, device="cuda"), torch.empty((a_rows, Kd // BLOCK), device="cuda")
     at = torch.linspace(a_rows - 1, 0, rows, device="cuda", dtype=torch.float64).long()

@@ -229,7 +229,7 @@ __device__ uint4 zero_piece;             // where pieces of tokens past the row'
 // Bounds.  Few rows: the weights' bytes, 4.5 TB/s at 128 rows of 4096 -> 14336 in 8 groups.  Many rows: the matrix units at the
 // clock that their power leaves.  14336 -> 4096 of 8192 rows: 537 us, 1.79 PFLOP/s (a library's product of 8192^3 in e4m3: 2.7).
 // With e4m3 widened, 4096 -> 14336 of 8192 rows: 1695 us, 1.14 PFLOP/s (in fp16: 1.59), the clock at 2.17 of 2.4 GHz; tiles of 128
-// rows with instructions of 32 x 32 took 3 % fewer cycles, at 1.93 GHz.
+// rows with instructions of 32 x 32 took 3 % fewer cycles, at 1.93 GHz, and were no faster.
 // Everything lies in one LDS array: of several, the compiler tells apart which one direct loads fill, and holds every read
 // of that one until no load is in flight.
 // ---------------------------------------------------------------------------------------------------------------------
@@ -607,13 +607,14 @@ __device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &
     const int row0 = t.row0, row_end = row0 + rows, n0 = t.nt * 32;      // the tile's rows, fewer than the matrix instruction's
     uint8_t *mine = ring + wave * (S * 4096);
 
-    const uint8_t *wp[4];
+    const uint8_t *const rows_at = b0 + (size_t)n0 * Kd;
+    uint32_t wo[4];
     const int piece = (lane & 7) ^ ((lane >> 4) & 3);             // of rows 8 j + lane / 8: (row >> 1) & 7 is 4 (j & 1) more
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int pos = j * 8 + (lane >> 3), b = pos >> 4, m = pos & 15;
-        const int n = min(n0 + (m >> 2) * 8 + b * 4 + (m & 3), N - 1);         // a lane's results: consecutive columns
-        wp[j] = b0 + (size_t)n * Kd + ((piece ^ (4 * (j & 1))) * 16);
+        const int n = min((m >> 2) * 8 + b * 4 + (m & 3), N - 1 - n0);         // a lane's results: consecutive columns
+        wo[j] = (uint32_t)n * (uint32_t)Kd + ((piece ^ (4 * (j & 1))) * 16);
     }
     const uint8_t *tp[TB];
 #pragma unroll
@@ -636,7 +637,7 @@ __device__ __forceinline__ void stream_tile(const ProductParams &p, const Tile &
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int pc = (piece ^ (4 * (j & 1))) * 16, back = k0 + pc >= Kd ? pc : 0;
-            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(wp[j] + (k0 - back)), (BM_LDS void *)(mine + st * 4096 + j * 1024), 16, 0, 0);
+            fetch<16>(rows_at, wo[j] - back, k0, mine + st * 4096 + j * 1024);
         }
 #pragma unroll
         for (int i = 0; i < TB; ++i) {

@@ -244,8 +244,8 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
     constexpr int PER = WI + TI + 1;                           // with the tokens' scales
     constexpr int AHEAD = ST < SW ? WI + (ST - 2) * PER : (ST - 2) * PER;
     constexpr int PART = BM <= 64 ? 1 : TB;                    // blocks that are multiplied or, where no token is theirs, left out together
-    constexpr bool SPREAD = BM > 64 && PER_UNIT == 1;           // loads are issued between the matrix instructions
-    static_assert(!SPREAD || PER <= TB * WB / 2, "places for loads");
+    // loads are issued between the matrix instructions, where these leave enough places
+    constexpr bool SPREAD = BM > 64 && PER_UNIT == 1 && PER <= (WIDE ? TB * 4 : TB * WB / 2);
     constexpr int MIN_STEPS = 4;                               // shorter walks are filled up with blocks of zeros
     static_assert(TB * 16 * WMN == BM && WB * 16 * WNN == BN && (TR >= 8 ? TR % 8 == 0 : TR > 0), "tile shape");
     static_assert(ST <= SW && SW <= MIN_STEPS && AHEAD < 64, "stages");
@@ -763,6 +763,9 @@ static void launch_stream(const ProductParams &p, hipStream_t st) {
 //   512: 208 240 298 433     64: 55 46 53 72        32: 46 36 35 43        16: 50 35 31 34        4: 33 21 20 19
 // Tiles of 128 rows: 256 columns for long reductions of 8-bit instructions (14336 -> 4096 of 1024 rows in 8 groups: 134 us against 147),
 // else 128 and two workgroups a unit (768 -> 2048 of 8192 rows in 128 groups: 46 against 49; of 512 rows, 14336 -> 4096 in fp32: 149 against 187).
+// Fewer than 256 tiles of 128 rows, but more of 64: a unit each and four stages (1000 x 2080 x 1440 in fp32 | bf16: 22.8 | 17.3 us against
+// 25.4 | 18.4 on 64 rows; 1800 x 2048 x 4096: 47.2 | 32.4 against 54.2 | 37.3; with 256 tiles of 64 rows these win, 512 x 4096 x 4096: 34.9
+// against 39.8).
 // Tiles of 32 rows: at 2048 -> .. and beyond the reduction is worth two parts within a workgroup (14336 -> 4096 of 16 rows: 56 us
 // against 69; of 512 rows, 768 -> 2048: 59 against 43).  Up to 128 tiles the streaming kernel takes 9.4 us for 1 x 4096 x 4096 against
 // 17, 18.5 for 64 x 1024 x 8192 against 34; with more it is even (58.6 against 60 for 16 rows of 14336 -> 4096 in 8 groups).
@@ -770,11 +773,13 @@ template <bool WIDE>
 static void launch_product_t(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
     auto tiles = [&](int bm, int bn) { return tiles_bound(p.rows, p.N, p.n_groups, bm, bn); };
+    const bool few_tiles = avg >= 128 && p.rows * (long long)((p.N + 127) / 128) > 256 * 64;
     const bool long_rows = !WIDE && p.Kd >= 4096 && avg >= 128 && tiles(128, 256) >= 256;
     if (avg >= 256 && tiles(192, 256) >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, false, WIDE>(p, st);
     else if (long_rows) {
         if constexpr (!WIDE) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, false, false>(p, st);
     } else if (avg >= 48 && tiles(128, 128) >= 256) launch_tiles<128, 128, 2, 4, 1, 2, 2, 2, false, WIDE>(p, st);
+    else if (few_tiles) launch_tiles<128, 128, 2, 4, 1, 4, 4, 1, false, WIDE>(p, st);
     else if (avg >= (p.Kd >= 2048 ? 32 : 16) && tiles(64, 128) >= 256) launch_tiles<64, 128, 2, 4, 1, 3, 3, 2, false, WIDE>(p, st);
     else if (p.Kd >= 2048 && tiles(32, 128) <= 128) launch_stream<WIDE>(p, st);
     else if (p.Kd >= 2048) launch_tiles<32, 128, 1, 4, 2, 3, 3, 1, false, WIDE>(p, st);

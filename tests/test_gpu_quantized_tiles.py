@@ -94,6 +94,7 @@ PRODUCTS = [
     ([600, 700], 8224, 512, 1), ([600, 0, 700], 8224, 480, 2), ([1300], 9472, 640, 1), ([1153], 9504, 96, 4),        # 192 x 256
     (SIXTY, 3200, 512, 1), (SIXTY, 3232, 2048, 8), (SIXTY, 3200, 352, 2), ([130] * 40, 1056, 768, 1),               # 128 x 128
     ([130] * 8, 4096, 4096, 1), ([140, 0, 260, 1, 129, 128, 255, 127], 4128, 4128, 2),                             # 128 x 256 in bf16
+    ([1000], 2080, 1440, 1), ([300, 280, 310, 290], 2048, 2048, 2), ([900], 2560, 512, 1), ([0, 299, 700], 2080, 96, 4),          # 128 x 128, a unit each
     (TWENTY, 3200, 512, 1), (TWENTY, 3232, 416, 4), (FORTY, 2816, 2176, 1), (FORTY, 2848, 2080, 2),                 # 64 x 128
     ([5], 160, 2048, 1), ([1], 4096, 4096, 1), ([17, 0, 33, 1], 96, 4128, 2), ([32], 512, 14336, 1),                # streamed
     ([9, 0, 1, 8], 64, 14464, 1), ([3, 12], 32, 32768, 1), ([1, 0, 2], 96, 14368, 3),                               # by eight rows

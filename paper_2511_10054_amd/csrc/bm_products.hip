@@ -793,17 +793,26 @@ int launch_product(const ProductParams &p, hipStream_t st) {
 }
 
 // As above, with 128 columns of both matrices a tile.  Measured in us, gate/up 4096 -> 14336 of 8 groups, rows a group and tiles
-// of 192 | 128 | 32 rows:   1024: 1695 . .    256: 534 549 731    128: 324 330 416    64: . 218 240    16: 186 169 130
+// of 192 | 128 | 32 rows:   1024: 1670 . .    256: 534 549 731    128: 324 330 416    64: . 218 240    16: 186 169 130
 // and 2048 -> 768 of 128 groups:   512: 472 490 670    128: . 153 198    64: . 110 104    32: 104 80 69
+// From 96 rows a group (64 for long reductions) the least of rounds over the units times what a step of 128 takes, in us (2.1 and 1.55 for
+// tiles of 192 and 128; of 32 rows 0.85, two on a unit 1.45), decides: 300 rows 4096 -> 4096 take 74 | 56 | 49 us, 1024 rows 81 | 67 | 102, 2000 rows
+// 2880 -> 2880 75 | 95 | 116, 4 groups of 300 rows 2048 -> 768 42 | 32 | 21.
 // Tiles of 32 rows: four stages and one workgroup a unit, or two and two.  The first wins where tiles are fewer than units (two rows,
 // 4096 -> 14336: 41 us against 49) and in the last round of long reductions, whose tiles have a unit each (4096 -> 8192, 640 tiles: 121
 // against 130, 768: 138 against 139, 1024: 183 against 182); the second where a second round would hold few tiles (2048 -> 768 of 512 rows in
-// 128 groups, half of them empty: 46 against 37) and with more rows a tile (4096 -> 14336 of 128 rows in 8 groups: 137 against 130).
+// 128 groups, half of them empty: 46 against 37) and with more rows a tile (4096 -> 14336 of 128 rows in 8 groups: 137 against 130; of one
+// group of 128 rows 72 against 54).
 int launch_swiglu(const ProductParams &p, hipStream_t st) {
     const long long avg = p.rows / p.n_groups;
-    if (avg >= 256) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, true, true>(p, st);
-    else if (avg >= (p.Kd >= 4096 ? 64 : 96)) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, true, true>(p, st);
-    else if (tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= (p.Kd >= 4096 ? 1024 : 512)) launch_tiles<32, 256, 1, 8, 1, 4, 4, 1, true, true>(p, st);
+    const double groups = p.n_groups < p.rows ? p.n_groups : p.rows, columns = (p.N + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    auto tiles = [&](int bm) { return ((double)p.rows / bm + 0.5 * groups) * columns; };      // half a tile of every group is no row
+    auto rounds = [](double tiles, int at_once) { return tiles > at_once ? tiles / at_once : 1.0; };
+    const double t32 = tiles(32) <= 256 ? 0.85 : 1.45 * rounds(tiles(32), 512), t128 = 1.55 * rounds(tiles(128), 256), t192 = 2.1 * rounds(tiles(192), 256);
+    const bool many = avg >= (p.Kd >= 4096 ? 64 : 96);
+    if (avg >= 256 && t192 <= t128 && t192 <= t32) launch_tiles<192, 256, 2, 4, 1, 3, 2, 1, true, true>(p, st);
+    else if (many && t128 <= t32) launch_tiles<128, 256, 2, 4, 1, 3, 3, 1, true, true>(p, st);
+    else if (avg < 32 && tiles_bound(p.rows, p.N, p.n_groups, 32, SCALE_BLOCK) <= (p.Kd >= 4096 ? 1024 : 512)) launch_tiles<32, 256, 1, 8, 1, 4, 4, 1, true, true>(p, st);
     else launch_tiles<32, 256, 1, 8, 1, 2, 2, 2, true, true>(p, st);
     return launch_status(__func__);
 }

@@ -126,8 +126,10 @@ def test_products_in_every_tile_shape(counts, N, Kd, K):
 
 
 EXPERTS = [
-    ([1300], 4864, 512, 1), ([300, 0, 700], 384, 640, 2), ([513, 140], 416, 1184, 3), ([300, 400, 500], 5024, 96, 1),            # 192 rows
-    ([130, 0, 300, 128], 1408, 512, 6), ([129, 200], 2080, 2048, 2), ([70, 1, 129], 160, 4096, 1), ([150, 90, 97], 96, 352, 1),  # 128 rows
+    ([1300], 4864, 512, 1), ([500, 0, 800], 4896, 640, 2), ([300, 400, 500], 5024, 96, 1), ([600, 710], 5024, 1184, 3),          # 192 rows
+    ([300, 250, 280], 4128, 512, 1), ([300, 250, 280], 4128, 352, 6), ([70, 1, 129, 90], 7200, 4096, 2),                         # 128 rows
+    ([300, 0, 700], 384, 640, 2), ([513, 140], 416, 1184, 3), ([130, 0, 300, 128], 1408, 512, 6), ([129, 200], 2080, 2048, 2),   # few tiles: 32 rows
+    ([70, 1, 129], 160, 4096, 1), ([150, 90, 97], 96, 352, 1), ([1000], 1408, 736, 1),
     ([2], 1408, 4096, 1), (mixed(16, 20, 11), 768, 2048, 8), (mixed(10, 60, 12), 416, 736, 2), ([33], 128, 32768, 1),             # 32 rows, four stages
     (mixed(64, 12, 13), 1152, 512, 1), (mixed(64, 40, 14), 1056, 608, 4), (mixed(128, 6, 15), 768, 2048, 8), (mixed(60, 9, 16), 1184, 96, 1),   # two
 ]

@@ -9,6 +9,7 @@
 // eight products that it adds at once below 2^-13 of the largest of them (measured: 1.4e-5 of the result's 2-norm, whatever
 // the instruction's shape): it serves results that are rounded to bf16.  Results in 32 bits - sums that stay so, and h, whose
 // scales are 32-bit numbers - widen e4m3 to fp16, which is exact, for v_mfma_f32_16x16x32_f16 at half the rate (7e-8).
+#include "bm_product_rings.h"
 #include "bm_products.h"
 
 namespace bm {
@@ -218,8 +219,10 @@ __device__ uint4 zero_piece;             // where pieces of tokens past the row'
 //
 // A workgroup takes one tile after the other and its loads run ahead across them: the last steps of a tile fetch the first
 // blocks of the next, whose rows and scales were fetched at the tile's beginning.  A step waits for the loads that it needs
-// and leaves those behind them in flight (AHEAD; loads return in order, and whatever else is in flight only makes the
-// wait stricter).
+// and leaves those behind them in flight (AHEAD; loads return in order).  Other loads in between make the wait stricter for these,
+// but are covered by it themselves only if as many of a step's loads follow them: the next tile's row ids, asked for in step 0,
+// are not where a walk is as short as four stages, and are then waited for by themselves (TileRings; 8 gathered rows in each of 64
+// groups, 512 -> 640: 15.9 us; 640 -> 640, which need no such wait: 17.6).
 //   step s:  tokens of step s and weights of step s have landed -> all waves meet (so the stages read in step s - 1 are
 //   free) -> load the tokens of step s + ST - 1 and the weights of step s + SW - 1 -> multiply.
 // NEAR: the reduction is a multiple of 128, at least MIN_STEPS blocks, and a is smaller than 4 GiB: no piece is cut, addresses are
@@ -239,16 +242,12 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
     constexpr int TB = BM / WMN / 16, WB = BN / WNN / 16;      // 16-token and 16-row blocks of a wave
     constexpr int HB = DUAL ? WB / 2 : WB;                     // of these, blocks of different columns
     constexpr int COLS = DUAL ? BN / 2 : BN;
-    constexpr int WI = BN / NW / 8;                            // weight loads of a wave and stage
-    constexpr int TR = BM / NW, TI = TR >= 8 ? TR / 8 : 1;     // token rows and loads of a wave and stage
-    constexpr int PER = WI + TI + 1;                           // with the tokens' scales
-    constexpr int AHEAD = ST < SW ? WI + (ST - 2) * PER : (ST - 2) * PER;
+    using Rings = TileRings<BM, BN, NW, SW, ST>;
+    constexpr int WI = Rings::WI, TR = Rings::TR, TI = Rings::TI, PER = Rings::PER, AHEAD = Rings::AHEAD;
     constexpr int PART = BM <= 64 ? 1 : TB;                    // blocks that are multiplied or, where no token is theirs, left out together
     // loads are issued between the matrix instructions, where these leave enough places
     constexpr bool SPREAD = BM > 64 && PER_UNIT == 1 && PER <= (WIDE ? TB * 4 : TB * WB / 2);
-    constexpr int MIN_STEPS = 4;                               // shorter walks are filled up with blocks of zeros
-    static_assert(TB * 16 * WMN == BM && WB * 16 * WNN == BN && (TR >= 8 ? TR % 8 == 0 : TR > 0), "tile shape");
-    static_assert(ST <= SW && SW <= MIN_STEPS && AHEAD < 64, "stages");
+    static_assert(TB * 16 * WMN == BM && WB * 16 * WNN == BN, "tile shape");
     constexpr int MAX_KB = MAX_PRODUCT_KD / SCALE_BLOCK;
     constexpr int W_BYTES = SW * KG * BN * 128, T_BYTES = ST * KG * BM * 128, EXCHANGE = KG > 1 ? (KG - 1) * NW * 1024 : 0;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[W_BYTES + T_BYTES + EXCHANGE + (ST * KG * BM + 4 * MAX_KB + BM + (DUAL ? WNN * BM : 0)) * 4 + sizeof(TileTable)];
@@ -390,7 +389,11 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
                 next = tile_at(p, tt, BM, n_nt, lid + share.step);
                 load_meta(next, buf ^ 1, true);
             }
-            if (more && step + ST - 1 == KT) aim_tokens(next, true);
+            if (more && step + ST - 1 == KT) {
+                if constexpr (Rings::ids_need_wait(MIN_STEPS))
+                    if (Rings::ids_need_wait(KT)) BM_WAIT_OWN(Rings::BEHIND_IDS)
+                aim_tokens(next, true);
+            }
             if (more && step + SW - 1 == KT) aim_weights(next);
             const int t_step = step + ST - 1 < KT ? step + ST - 1 : step + ST - 1 - KT, w_step = step + SW - 1 < KT ? step + SW - 1 : step + SW - 1 - KT;
             const int t_fill = t_slot, w_fill = w_slot;
@@ -743,7 +746,7 @@ static void launch_tiles(const ProductParams &p, hipStream_t st) {
     const long long tiles = (tiles_bound(p.rows, p.N, p.n_groups, BM, DUAL ? BN / 2 : BN) + 7) / 8 * 8;
     const dim3 grid((unsigned)(tiles < 256 * PER_UNIT ? tiles : 256 * PER_UNIT)), block(WMN * WNN * KG * 64);
     // 32-bit offsets into a, whole steps (see tiles_kernel)
-    const bool near = p.Kd % (KG * SCALE_BLOCK) == 0 && p.Kd >= 4 * KG * SCALE_BLOCK && (long long)p.a_rows * p.Kd < (1ll << 32);
+    const bool near = p.Kd % (KG * SCALE_BLOCK) == 0 && p.Kd >= MIN_STEPS * KG * SCALE_BLOCK && (long long)p.a_rows * p.Kd < (1ll << 32);
     if (near) hipLaunchKernelGGL((tiles_kernel<BM, BN, WMN, WNN, KG, SW, ST, PER_UNIT, DUAL, WIDE, true>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((tiles_kernel<BM, BN, WMN, WNN, KG, SW, ST, PER_UNIT, DUAL, WIDE, false>), grid, block, 0, st, p);
 }

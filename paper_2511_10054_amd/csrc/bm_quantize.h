@@ -16,10 +16,10 @@ __device__ __forceinline__ float block_scale(uint32_t max_bits) {
 
 // x / s rounded to 32 bits, from inv = 1 / s: the product with the reciprocal is within two units in the last place, one
 // step of the remainder makes it the rounded quotient.  Without it 16-bit inputs, whose quotients often lie exactly half way
-// between two e4m3 values, fall to either side.
+// between two e4m3 values, fall to either side.  The remainder is taken as y s - x, so that -0 stays -0.
 __device__ __forceinline__ float quotient(float x, float s, float inv) {
     const float y = x * inv;
-    return fmaf(fmaf(-y, s, x), inv, y);
+    return fmaf(-fmaf(y, s, -x), inv, y);
 }
 
 // Four values (magnitudes up to 448) to e4m3, rounded to nearest even, the first in the lowest byte

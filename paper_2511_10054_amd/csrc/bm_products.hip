@@ -567,14 +567,17 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
 #pragma unroll
                 for (int w = 0; w < WNN; ++w) m = max(m, s_amax[w * BM + at]);
                 if (kg > 0 || r >= cur.row_end) continue;
-                const float s = block_scale(m), inv = 1.0f / s;
+                const float s = block_scale(m);
+                const Divisor by = divisor(s);
                 if (wn == 0 && q4 == 0) p.c_scale[(size_t)r * nb_n + cur.nt] = s;
                 if (!in) continue;
                 uint8_t *c = static_cast<uint8_t *>(p.c) + (size_t)r * N + col;
 #pragma unroll
-                for (int b = 0; b < HB; ++b)
-                    *(BM_GLOBAL uint32_t *)(c + 4 * b) = e4m3x4(quotient(acc[b][i][0], s, inv), quotient(acc[b][i][1], s, inv),
-                                                                quotient(acc[b][i][2], s, inv), quotient(acc[b][i][3], s, inv));
+                for (int b = 0; b < HB; ++b) {
+                    float v[4] = {acc[b][i][0], acc[b][i][1], acc[b][i][2], acc[b][i][3]};
+                    raise(v, by);
+                    *(BM_GLOBAL uint32_t *)(c + 4 * b) = e4m3x4(quotient(v[0], by), quotient(v[1], by), quotient(v[2], by), quotient(v[3], by));
+                }
             }
         }
         if (!more) {

@@ -42,13 +42,14 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const T *src, uint
     if ((tid & 63) == 0) s_max[tid >> 6] = m;
     __syncthreads();
     m = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-    const float s = block_scale(m), inv = 1.0f / s;
+    const float s = block_scale(m);
+    const Divisor by = divisor(s);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = r0 + 16 * i;
         float f[8];
         v[i].get(f);
-        if (r < rows && j < cols) store_q8<ALIGNED>(q + base + (size_t)r * cols + j, cols - j, f, s, inv);
+        if (r < rows && j < cols) store_q8<ALIGNED>(q + base + (size_t)r * cols + j, cols - j, f, by);
     }
     if (tid == 0) scale[((size_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x] = s;
 }
@@ -105,8 +106,8 @@ __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(NormParams p) {
             // lanes past the row's end hold gamma = 0 and may have 0 * infinity there: they are left out
             const uint32_t m = row16_max_u32(j < d ? max_bits(v[i], 0) : 0u);
             if (j < d) {
-                const float s = block_scale(m), inv = 1.0f / s;
-                store_q8<ALIGNED>(p.q + at + j, d - j, v[i], s, inv);
+                const float s = block_scale(m);
+                store_q8<ALIGNED>(p.q + at + j, d - j, v[i], divisor(s));
                 if ((tid & 15) == 0) p.scale[(size_t)blockIdx.x * kb + j / SCALE_BLOCK] = s;
             }
         }

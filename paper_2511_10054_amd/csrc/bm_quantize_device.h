@@ -76,9 +76,10 @@ __device__ __forceinline__ void store8(T *p, int n, const float (&v)[8]) {
 }
 
 template <bool ALIGNED>
-__device__ __forceinline__ void store_q8(uint8_t *p, int n, const float (&v)[8], float s, float inv) {
-    const uint32_t lo = e4m3x4(quotient(v[0], s, inv), quotient(v[1], s, inv), quotient(v[2], s, inv), quotient(v[3], s, inv));
-    const uint32_t hi = e4m3x4(quotient(v[4], s, inv), quotient(v[5], s, inv), quotient(v[6], s, inv), quotient(v[7], s, inv));
+__device__ __forceinline__ void store_q8(uint8_t *p, int n, float (&v)[8], const Divisor &s) {
+    raise(v, s);
+    const uint32_t lo = e4m3x4(quotient(v[0], s), quotient(v[1], s), quotient(v[2], s), quotient(v[3], s));
+    const uint32_t hi = e4m3x4(quotient(v[4], s), quotient(v[5], s), quotient(v[6], s), quotient(v[7], s));
     if (ALIGNED) {
         const u32x2 u = {lo, hi};
         *(BM_GLOBAL u32x2 *)p = u;
@@ -144,10 +145,10 @@ __device__ __forceinline__ void quantize_row_block(const T *src, uint8_t *q, flo
     if (in) v.template load<ALIGNED>(src + at, cols - j);
     const uint32_t m = row16_max_u32(v.max_of());
     if (!in) return;
-    const float s = block_scale(m), inv = 1.0f / s;
+    const float s = block_scale(m);
     float f[8];
     v.get(f);
-    store_q8<ALIGNED>(q + at, cols - j, f, s, inv);
+    store_q8<ALIGNED>(q + at, cols - j, f, divisor(s));
     if ((threadIdx.x & 15) == 0) scale[blk] = s;
 }
 

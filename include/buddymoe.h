@@ -324,8 +324,8 @@ typedef struct {
 /* q [n][rows][cols] and scale [n][rows / block_rows, rounded up][ceil(cols/128)] of
  * src [n][rows][cols] (all device).  Weights are quantized once, at load time; any
  * width is taken, whole 16-byte pieces at a time where cols is a multiple of 8 and the
- * arrays are aligned; fewer than 2^28 - 16 blocks of rows, or
- * up to 65535 matrices of 65535 rows of blocks. */
+ * arrays are aligned; up to 2^28 - 16 blocks of rows, or
+ * up to 65535 matrices of 65535 rows of fewer than 2^24 blocks (BM_ERR_SHAPE beyond). */
 int bm_quantize(const bm_quantize_desc *desc, const void *src, void *q, float *scale, void *stream);
 
 typedef struct {

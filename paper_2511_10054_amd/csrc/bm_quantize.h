@@ -59,7 +59,8 @@ struct NormParams {
 // the launch's grid stays within its limits
 inline bool quantize_grid_ok(int n, int rows, int cols, bool blocks) {
     const long long kb = ((long long)cols + SCALE_BLOCK - 1) / SCALE_BLOCK, rb = ((long long)rows + SCALE_BLOCK - 1) / SCALE_BLOCK;
-    return blocks ? rb <= 65535 && n <= 65535 : (long long)n * rows <= ((1ll << 28) - 16) / kb;      // 16 threads a block, under 2^32 a launch
+    return blocks ? rb <= 65535 && n <= 65535 && kb < (1ll << 24)                   // 256 threads a block, under 2^32 along each side
+                  : (long long)n * rows <= ((1ll << 28) - 16) / kb;                  // 16 threads a block, under 2^32 a launch
 }
 
 // Threads of a norm's workgroup: eight values each, in whole waves, twice eight past 8192

@@ -135,7 +135,7 @@ int launch_add_rmsnorm(const NormParams &p, bool f32, hipStream_t st) {
 template <typename T>
 static void launch_quantize_t(const void *src, uint8_t *q, float *scale, int n, int rows, int cols, bool blocks, hipStream_t st) {
     const bool al = cols % 8 == 0 && aligned16(src) && ((uintptr_t)q & 7) == 0;
-    const int kb = (cols + SCALE_BLOCK - 1) / SCALE_BLOCK;
+    const int kb = cols / SCALE_BLOCK + (cols % SCALE_BLOCK != 0);       // (the sum of cols and 127 can pass 2^31)
     const T *s = static_cast<const T *>(src);
     if (blocks) {
         const dim3 grid(kb, (rows + SCALE_BLOCK - 1) / SCALE_BLOCK, n);

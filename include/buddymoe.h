@@ -329,7 +329,8 @@ typedef struct {
 int bm_quantize(const bm_quantize_desc *desc, const void *src, void *q, float *scale, void *stream);
 
 typedef struct {
-    int32_t T, d;            /* rows and width, 1 <= d <= 16384, T * d / 8 under 2^32        */
+    int32_t T, d;            /* rows and width, 1 <= d <= 16384; T * lanes under 2^32, where
+                                lanes is d / 8 rounded up to whole 64s, at most 1024     */
     int32_t dtype;           /* of x, residual, gamma, residual_out, y: BM_F32 or BM_BF16    */
     float eps;               /* >= 0, added to the mean square                               */
 } bm_norm_desc;

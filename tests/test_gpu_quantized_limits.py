@@ -25,3 +25,23 @@ def test_quantize_of_the_longest_row(cols):
     # zeros between, each with the smallest scale
     assert int(q.view(-1)[1024:cut].max()) == 0
     assert bool((s[0, 8:cut // BLOCK] == 2.0 ** -126).all())
+
+
+@pytest.mark.parametrize("T,d", [((1 << 26) - 1, 8), ((1 << 25) - 1, 513), ((1 << 22) - 1, 8200)])
+def test_norm_of_the_most_rows(T, d):
+    """One row less than is refused: the first and the last rows, and nothing else than zeros between."""
+    print("most rows", T, d, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.zeros((T, d), dtype=torch.bfloat16, device="cuda")
+    for lo in (0, T - 300):
+        x[lo:lo + 300] = torch.randn((300, d), generator=g, device="cuda").bfloat16()
+    w = (1.0 + 0.2 * torch.randn(d, generator=g, device="cuda")).bfloat16()
+    y = torch.full_like(x, 7.0)
+    bm.bm_add_rmsnorm(bm.NormDesc(T=T, d=d, dtype=bm.BM_BF16, eps=1e-5), x, None, w, y=y)
+    for lo in (0, T - 300):
+        t = x[lo:lo + 300].double()
+        want = t / (t.square().mean(1, keepdim=True) + 1e-5).sqrt() * w.double()
+        # bf16's half step; the 32-bit sum of squares and quotient are far below a hundredth of it
+        assert bool(((y[lo:lo + 300].double() - want).abs() <= 2.0 ** -8 * 1.01 * want.abs()).all())
+    for part in y[300:T - 300].split(1 << 22):
+        assert not bool(part.any())

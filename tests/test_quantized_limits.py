@@ -1,6 +1,7 @@
 """Sizes at the ends of the 8-bit operators' ranges, on the host: what is past them is refused before anything is launched (CPU
 only)."""
 import ctypes
+import os
 
 import pytest
 
@@ -18,3 +19,17 @@ SHAPE = -2
 def test_quantize_refuses_grids_past_the_launch(n, rows, cols, block):
     d = bm.QuantizeDesc(n=n, rows=rows, cols=cols, block_rows=block, dtype=bm.BM_BF16)
     assert bm.load_library().bm_quantize(ctypes.byref(d), ONE, ONE, ONE, None) == SHAPE
+
+
+# lanes: eight values each in whole waves of 64, at most 1024
+@pytest.mark.parametrize("T,d", [(1 << 26, 1), (1 << 26, 8), (1 << 26, 512), (1 << 25, 513), (1 << 25, 1024), (1 << 22, 8192), (1 << 22, 8193), (1 << 22, 16384)])
+def test_norm_refuses_grids_past_the_launch(T, d):
+    desc = bm.NormDesc(T=T, d=d, dtype=bm.BM_BF16, eps=0.0)
+    assert bm.load_library().bm_add_rmsnorm(ctypes.byref(desc), ONE, ONE, ONE, None, ONE, None, None, None) == SHAPE
+
+
+def test_header_states_the_norms_limit():
+    """The header's text, in numbers, at both sides of what the call above refuses."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "buddymoe.h")) as f:
+        text = " ".join(f.read().split())
+    assert "T * lanes under 2^32, where lanes is d / 8 rounded up to whole 64s, at most 1024" in text

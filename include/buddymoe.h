@@ -346,9 +346,10 @@ int bm_add_rmsnorm(const bm_norm_desc *desc, const void *x, const void *residual
                    void *residual_out, void *y, void *q, float *scale, void *stream);
 
 typedef struct {
-    int32_t rows;            /* rows of the output, at least offsets[E]                      */
+    int32_t rows;            /* rows of the output, at least offsets[E]; at most 2^30        */
     int32_t a_rows;          /* rows of a                                                    */
-    int32_t N, Kd;           /* output width and reduction, multiples of 32, Kd <= 32768     */
+    int32_t N, Kd;           /* output width and reduction, multiples of 32, N <= 2^20,
+                                Kd <= 32768; (rows / 8 + E) * N / 32 under 2^31 - 8      */
     int32_t E;               /* groups, 1 <= E <= BM_MAX_E                                   */
     int32_t K;               /* output row i reads row row_map[i] / K of a                   */
     int32_t dtype;           /* of c: BM_F32 or BM_BF16 (not read by bm_grouped_swiglu)      */
@@ -404,7 +405,8 @@ typedef struct {
  * from x.  Every expert's output is held in fp32 up to 256 tokens and in bf16 beyond.
  * workspace: device scratch, 256-byte aligned, of at least
  * bm_workspace_bytes_quantized(desc) bytes (one sized for a larger T of the layer is
- * enough).  d and F at most 32768.  Equal calls give equal bits; a token's y can differ
+ * enough).  d and F at most 32768, T * (K + n_shared) rows at most 2^30 and with d and F
+ * within bm_product_desc's limits, T rows of d within bm_quantize's.  Equal calls give equal bits; a token's y can differ
  * in its last bits with the rest of the batch. */
 int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale,
                              const bm_quantized_weights *weights, const uint64_t *residency_bitmap,

@@ -392,7 +392,9 @@ int check_quantized_desc(const bm_layer_desc *d) {
     if (rc) return rc;
     if (d->dtype != BM_BF16) return BM_ERR_DTYPE;
     if (d->d > MAX_PRODUCT_KD || d->F > MAX_PRODUCT_KD) return BM_ERR_SHAPE;
-    if ((long long)d->T * (d->K + d->n_shared) > (1ll << 30) || !quantize_grid_ok(1, d->T, d->d, false)) return BM_ERR_SHAPE;
+    const long long rows = (long long)d->T * (d->K + d->n_shared);
+    if (rows > (1ll << 30) || !quantize_grid_ok(1, d->T, d->d, false)) return BM_ERR_SHAPE;
+    if (!product_grid_ok(rows, d->d > d->F ? d->d : d->F, d->E + d->n_shared)) return BM_ERR_SHAPE;
     return BM_OK;
 }
 
@@ -861,7 +863,6 @@ int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const voi
     if (rc) return rc;
     const int T = desc->T, K = desc->K, E = desc->E, G = E + desc->n_shared;
     if (T == 0) return BM_OK;
-    if (!product_grid_ok((long long)T * (K + desc->n_shared), desc->d > desc->F ? desc->d : desc->F, G)) return BM_ERR_SHAPE;
     if (!x || !wt || !residency_bitmap || !y || (!buddy_table && desc->R > 0) || !x_q != !x_scale) return BM_ERR_NULL;
     if (!wt->w_router || !wt->w_gate || !wt->gate_scale || !wt->w_up || !wt->up_scale || !wt->w_down || !wt->down_scale) return BM_ERR_NULL;
     if (desc->n_shared > 0 && (!wt->ws_gate || !wt->ws_gate_scale || !wt->ws_up || !wt->ws_up_scale || !wt->ws_down || !wt->ws_down_scale))

@@ -366,10 +366,11 @@ typedef struct {
  * parts that depend on the sizes; c is rounded once.  The two scales of a block are
  * multiplied first: their product has to lie within fp32's normal range.  With c in bf16
  * the matrix unit may cut each of the eight products that it adds at once below 2^-13 of
- * the largest (1.4e-5 of a result's 2-norm, far under its rounding).  Rows of c behind
- * offsets[E] are left as they were, groups without rows read nothing.  Offsets are taken
- * as clamped to [0, rows] and no smaller than those before them, mapped rows as clamped
- * to [0, a_rows).  Equal calls give equal bits. */
+ * the largest: 1.4e-5 of a result's 2-norm, far under its rounding.  It cuts magnitudes:
+ * where all products have one sign, results are too small by up to 7e-5 of themselves on
+ * average.  Rows of c behind offsets[E] are left as they were, groups without rows read
+ * nothing.  Offsets are taken as clamped to [0, rows] and no smaller than those before
+ * them, mapped rows as clamped to [0, a_rows).  Equal calls give equal bits. */
 int bm_grouped_matmul(const bm_product_desc *desc, const void *a, const float *a_scale, const int32_t *row_map,
                       const int32_t *offsets, const void *w, const float *w_scale, void *c, void *stream);
 

@@ -403,7 +403,8 @@ typedef struct {
  * bm_grouped_swiglu and bm_grouped_matmul.  desc->dtype is BM_BF16 (of x, w_router and,
  * without BM_Y_F32, y).  x_q [T][d], x_scale [T][ceil(d/128)]: the 8-bit form of the
  * tokens that the experts read, as bm_add_rmsnorm writes it; both NULL: the call makes it
- * from x.  Every expert's output is held in fp32 up to 256 tokens and in bf16 beyond.
+ * from x.  Every expert's output is held in fp32 up to 256 tokens and in bf16 beyond, with
+ * BM_Y_F32 too (the flag is y's type alone, as in bm_moe_forward).
  * workspace: device scratch, 256-byte aligned, of at least
  * bm_workspace_bytes_quantized(desc) bytes (one sized for a larger T of the layer is
  * enough).  d and F at most 32768, T * (K + n_shared) rows at most 2^30 and with d and F

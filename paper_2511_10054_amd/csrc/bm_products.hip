@@ -230,10 +230,12 @@ __device__ uint4 zero_piece;             // where pieces of tokens past the row'
 // 32-bit offsets (which leaves room for tiles of 192 tokens).
 // SPREAD (128 and 192 rows): the loads of a step stand between its matrix instructions.  Issued together they held a wave for 900 of
 // 6300 cycles, since a unit takes 64 bytes a cycle of them.  Past the last tile they fetch the tile's beginning once more.
-// Bounds.  Few rows: the weights' bytes, 4.5 TB/s at 128 rows of 4096 -> 14336 in 8 groups.  Many rows: the matrix units at the
-// clock that their power leaves.  14336 -> 4096 of 8192 rows: 537 us, 1.79 PFLOP/s (a library's product of 8192^3 in e4m3: 2.7).
-// With e4m3 widened, 4096 -> 14336 of 8192 rows: 1695 us, 1.14 PFLOP/s (in fp16: 1.59), the clock at 2.17 of 2.4 GHz; tiles of 128
-// rows with instructions of 32 x 32 took 3 % fewer cycles, at 1.93 GHz, and were no faster.
+// Bounds.  Few rows: the weights' bytes, read once, 4.6 TB/s at 128 rows of 4096 -> 14336 in 8 groups.  Many rows: the matrix units at
+// the clock that their power leaves.  14336 -> 4096 of 8192 rows: 531 us, 1.81 PFLOP/s (a library's product of 8192^3 in e4m3: 2.7).
+// With e4m3 widened, 4096 -> 14336 of 8192 rows: 1637 us, 1.17 PFLOP/s (in fp16: 1.59), matrix units busy 57 % of the cycles and vector
+// units 62 %, the clock at 2.17 of 2.4 GHz; tiles of 128 rows with instructions of 32 x 32 took 3 % fewer cycles, at 1.93 GHz, and were no
+// faster.  What is spilled (13 registers of the 192 x 256 gate/up form, 19 of its form with cut blocks, 1 to 6 of three products) is read
+// again where a tile ends or the next begins, never in a step.
 // Everything lies in one LDS array: of several, the compiler tells apart which one direct loads fill, and holds every read
 // of that one until no load is in flight.
 // ---------------------------------------------------------------------------------------------------------------------
@@ -508,7 +510,7 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
                             add(n - 2);
                             add(n - 1);
                         }
-                            }
+                    }
                     add(PART * WB - 2);
                     add(PART * WB - 1);
                 }
@@ -597,8 +599,8 @@ __global__ void __launch_bounds__(WMN * WNN * KG * 64, WMN * WNN * KG * PER_UNIT
 // consecutive lines, and the parts are added in order at the end.
 // Tokens go straight to registers, as far ahead as the weights: loads return in order, and waiting for a nearer one would
 // wait for all weights in flight.  Their scales lie in LDS from the start (from memory in the loop they cost as many bytes
-// from the L2 as the tokens: a line for four).  Measured at 1 row, 4096 -> 4096: 9.4 us, of which 5 are the launch and the first
-// and last bytes' way; 14336 -> 4096, two groups of one row: 21.7 us, 5.4 TB/s.
+// from the L2 as the tokens: a line for four).  Measured at 1 row, 4096 -> 4096: 8.5 to 9.4 us, of which 5 are the launch and the first
+// and last bytes' way; 14336 -> 4096, two groups of one row: 21.7 to 23.3 us, 5.0 to 5.4 TB/s.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int STREAM_WAVES = 4;
 constexpr int STREAM_SCALES = 32 * 112;          // tokens x blocks of 128 whose scales fit beside the ring

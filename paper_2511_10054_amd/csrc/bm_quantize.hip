@@ -10,7 +10,7 @@ namespace bm {
 
 // ---------------------------------------------------------------------------------------------------------------------
 // A scale for each 128 values of a row: 16 lanes of eight values each hold a block.  Bound by HBM, by the launch where rows are
-// few: 16384 x 4096 of bf16 5.4 TB/s; 4095 x 1440 6.2 us, of which the launch is 3.
+// few: 16384 x 4096 of bf16 5.2 to 5.4 TB/s; 4095 x 1440 of fp32 6.3 us, of which the launch is 3.
 // ---------------------------------------------------------------------------------------------------------------------
 template <bool ALIGNED, typename T>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *src, uint8_t *q, float *scale, long long n_rows, int cols, int kb) {
@@ -20,7 +20,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const T *src, uint8_
 // ---------------------------------------------------------------------------------------------------------------------
 // A scale for each 128 x 128 block of a matrix: one workgroup a block, its 16384 values in registers between the
 // search for the largest and the conversion (16-bit ones packed).  Bound by HBM: 16 x 1408 x 2048 of bf16 in 29 us, 4.8 TB/s, larger
-// ones up to 5.7 (a copy, with as many bytes written as read: 5.1).
+// ones up to 5.7, 4 x 4096 x 4096 of fp32 in 60 us, 5.6 (a copy, with as many bytes written as read: 5.1).
 // ---------------------------------------------------------------------------------------------------------------------
 template <bool ALIGNED, typename T>
 __global__ void __launch_bounds__(256) quantize_blocks_kernel(const T *src, uint8_t *q, float *scale, int rows, int cols) {
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const T *src, uint
 // r = x + residual, n = r / sqrt(mean(r^2) + eps) * gamma, in 32 bits; r and n are rounded once where they are written,
 // n's 8-bit form is made from the 32-bit values.  One workgroup a row, which stays in registers (NIT pieces of eight
 // values a thread) between the sum and the outputs: every input is read once.  Bound by HBM: 8192 x 2048 of bf16 with all outputs
-// in 31 us, 4.9 TB/s; one row by the launch and two trips to memory, 5.6 us.
+// in 31 us, 4.9 TB/s, 8192 x 4096 of fp32 in 103 us, 5.6 TB/s; one row by the launch and two trips to memory, 5.6 us.
 // ---------------------------------------------------------------------------------------------------------------------
 template <bool ALIGNED, typename T, int NIT>
 __global__ void __launch_bounds__(1024) add_rmsnorm_kernel(NormParams p) {

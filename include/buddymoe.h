@@ -83,6 +83,8 @@ enum {
 #define BM_MAX_E 256
 #define BM_MAX_K 32
 #define BM_MAX_R 32
+#define BM_MAX_ADAPTERS 1024
+#define BM_MAX_RANK 128
 
 typedef struct {
     int32_t T, d, E, F, K;
@@ -417,6 +419,93 @@ int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const voi
 
 /* Its scratch (host, pure function of desc; 0 if desc is invalid). */
 size_t bm_workspace_bytes_quantized(const bm_layer_desc *desc);
+
+/* ---- routing by scores, and the layer behind another router ------------------- */
+
+typedef enum { BM_SCORE_SOFTMAX = 0, BM_SCORE_SIGMOID = 1 } bm_scoring;
+
+typedef struct {
+    int32_t T, d, E, K;      /* as in bm_layer_desc; d at most 2^20                          */
+    int32_t n_groups;        /* equal groups of E / n_groups neighbouring experts, at most 64;
+                                1: no groups                                               */
+    int32_t keep_groups;     /* groups that a token chooses from, 1 to n_groups;
+                                K <= keep_groups * E / n_groups                            */
+    int32_t group_top;       /* a group's score is the sum of its 1 or 2 largest choices   */
+    int32_t scoring;         /* bm_scoring                                                 */
+    int32_t dtype;           /* of x and w_router: BM_F32, or BM_BF16 with d a multiple of 32 */
+    uint32_t flags;          /* BM_RENORM_TOPK                                             */
+    float scale;             /* factor of the weights, finite                              */
+} bm_router_desc;
+
+/* Routing by scores, with a bias for balance and groups of experts:
+ *   z[t][e] = bias[e] + sum_j x[t][j] * w_router[e][j]      (fp32 accumulation)
+ *   s = softmax(z) over all E, or 1 / (1 + exp(-z));   c = s + balance[e]
+ * A group's score is the sum of its group_top largest c; the keep_groups groups of
+ * largest score stay, equal scores the lower group.  ids[t][0..K) = the K experts of
+ * largest c in them, slot 0 the largest, equal c to the lower index; w[t][k] = s of
+ * slot k, without the balance, with BM_RENORM_TOPK divided by the K slots' sum (by
+ * 2^-126 where that is larger), times scale.  An expert whose c is -infinity or NaN
+ * is never chosen (a balance of -infinity switches it off): slots without an
+ * expert get id -1 and w 0, which bm_buddy_remap and the layer drop.
+ * x [T][d], w_router [E][d] (bf16: 16-byte aligned, BM_ERR_ALIGN otherwise), bias and
+ * balance [E] fp32 or NULL, ids [T][K] int32 and w [T][K] fp32 (written), all device.
+ * A token's ids and w are the same bits whatever T it is part of.  workspace: device
+ * scratch, 256-byte aligned, of at least bm_workspace_bytes_scored(desc) bytes (one
+ * sized for a larger T is enough as well).  T == 0 is a no-op. */
+int bm_route_scored(const bm_router_desc *desc, const void *x, const void *w_router, const float *bias,
+                    const float *balance, int32_t *ids, float *w, void *workspace, size_t workspace_bytes,
+                    void *stream);
+size_t bm_workspace_bytes_scored(const bm_router_desc *desc);   /* host; 0 if desc is invalid */
+
+/* bm_moe_forward and bm_moe_forward_quantized on a routing that the caller has:
+ * substitution, grouping, experts and aggregation, with the same gates (they read the
+ * weights renormalised to sum 1), workspace and results.  ids [T][K] int32, w [T][K] fp32
+ * (device, not written; ids outside [0,E) are dropped, one listed twice counts twice).
+ * w_router and router_bias of the weights are not read and may be NULL, nor is x of the
+ * 8-bit layer when x_q is given.  BM_RENORM_TOPK is not read.  BM_PSI_TOKEN needs the
+ * router's probabilities and is refused (BM_ERR_SHAPE).  dbg->ids gets ids as given. */
+int bm_moe_forward_routed(const bm_layer_desc *desc, const void *x, const int32_t *ids, const float *w,
+                          const bm_weights *weights, const uint64_t *residency_bitmap,
+                          const int32_t *buddy_table, void *y, void *workspace, size_t workspace_bytes,
+                          const bm_debug_out *dbg, void *stream);
+int bm_moe_forward_routed_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale,
+                                    const int32_t *ids, const float *w, const bm_quantized_weights *weights,
+                                    const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y,
+                                    void *workspace, size_t workspace_bytes, const bm_debug_out *dbg, void *stream);
+
+/* ---- low-rank adapters --------------------------------------------------------- */
+
+typedef struct {
+    int32_t rows;            /* of x, base and y, at most 2^24                             */
+    int32_t Kd, N;           /* widths of x and of y, at most 2^20                         */
+    int32_t n;               /* adapters in the arrays, 1 to BM_MAX_ADAPTERS               */
+    int32_t rank;            /* of the arrays, 1 to BM_MAX_RANK                            */
+    int32_t x_stride, base_stride, y_stride;  /* values from row to row; 0: the width      */
+    int32_t dtype;           /* of x, a and b: BM_F32 or BM_BF16                           */
+    int32_t y_dtype;         /* of base and y: BM_F32 or BM_BF16                           */
+} bm_adapter_desc;
+
+/* The low-rank adapters of many requests beside a shared projection (whose output is
+ * base: bm_grouped_matmul's c, or any other product's):
+ *   y[i] = base[i] + scale[s] * b[s] (a[s] x[i]),   s = adapter[i]
+ * x [rows][Kd], adapter [rows] int32, a [n][rank][Kd], b [n][N][rank], scale [n] fp32
+ * (NULL: 1), base and y [rows][N] (all device).  ranks [n] int32 (device, NULL: rank for
+ * all) is each adapter's own rank, taken as clamped to [0, rank]: values of a and b behind
+ * it do not count, whatever they are.  Rows whose adapter lies outside [0, n) get
+ * y = base.  base may be y (the same stride): such rows are then neither read nor
+ * written; otherwise base, x and y must not overlap.  Rows of a strided array keep what
+ * lies between them.
+ * Any sizes, strides and addresses are taken (4-byte addresses in fp32, 2-byte ones in
+ * bf16); 16 bytes at a time where rows and addresses are multiples of that.
+ * Sums are fp32, a x is held in fp32 (bf16: where b multiplies it, as the sum of three bf16
+ * values, its 24 bits, or for a bf16 y of two); y is rounded once.  Equal calls give equal bits; a row's y can differ in
+ * its last bits with rows and n.
+ * workspace: device scratch, 256-byte aligned, of at least
+ * bm_workspace_bytes_adapters(desc) bytes.  rows == 0 is a no-op. */
+int bm_add_adapters(const bm_adapter_desc *desc, const void *x, const int32_t *adapter, const void *a,
+                    const void *b, const int32_t *ranks, const float *scale, const void *base, void *y,
+                    void *workspace, size_t workspace_bytes, void *stream);
+size_t bm_workspace_bytes_adapters(const bm_adapter_desc *desc);   /* host; 0 if desc is invalid */
 
 /* Host-side check of a residency bitmap and buddy table (host pointers):
  * every table entry is -1 or in [0,E) and differs from its row index

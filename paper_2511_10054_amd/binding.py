@@ -13,6 +13,7 @@ _lib = None
 BM_F32, BM_BF16 = 0, 1
 BM_RENORM_TOPK, BM_REMAP_UNIQUE, BM_Y_F32 = 1, 2, 4
 BM_GATE_TAE, BM_GATE_MARGIN, BM_REPLACE_BUDGET, BM_GATE_DIST, BM_PSI_TOKEN = 8, 16, 32, 64, 128
+BM_SCORE_SOFTMAX, BM_SCORE_SIGMOID = 0, 1
 
 
 class BuddyMoEError(RuntimeError):
@@ -59,6 +60,16 @@ class QuantizedWeights(ctypes.Structure):
                  "ws_gate", "ws_gate_scale", "ws_up", "ws_up_scale", "ws_down", "ws_down_scale", "buddy_q")]
 
 
+class RouterDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "d", "E", "K", "n_groups", "keep_groups", "group_top", "scoring", "dtype")] + \
+               [("flags", ctypes.c_uint32), ("scale", ctypes.c_float)]
+
+
+class AdapterDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("rows", "Kd", "N", "n", "rank", "x_stride", "base_stride", "y_stride", "dtype", "y_dtype")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -102,6 +113,17 @@ def load_library() -> ctypes.CDLL:
                                                  vp, vp, ctypes.c_size_t, ctypes.POINTER(DebugOut), vp]
         lib.bm_workspace_bytes_quantized.restype = ctypes.c_size_t
         lib.bm_workspace_bytes_quantized.argtypes = [ctypes.POINTER(LayerDesc)]
+        lib.bm_route_scored.argtypes = [ctypes.POINTER(RouterDesc)] + [vp] * 7 + [ctypes.c_size_t, vp]
+        lib.bm_moe_forward_routed.argtypes = [ctypes.POINTER(LayerDesc), vp, vp, vp, ctypes.POINTER(Weights), vp, vp, vp, vp,
+                                              ctypes.c_size_t, ctypes.POINTER(DebugOut), vp]
+        lib.bm_moe_forward_routed_quantized.argtypes = [ctypes.POINTER(LayerDesc)] + [vp] * 5 + [ctypes.POINTER(QuantizedWeights)] + \
+            [vp] * 4 + [ctypes.c_size_t, ctypes.POINTER(DebugOut), vp]
+        lib.bm_add_adapters.argtypes = [ctypes.POINTER(AdapterDesc)] + [vp] * 9 + [ctypes.c_size_t, vp]
+        for f, desc in ((lib.bm_workspace_bytes_scored, RouterDesc), (lib.bm_workspace_bytes_adapters, AdapterDesc)):
+            f.restype = ctypes.c_size_t
+            f.argtypes = [ctypes.POINTER(desc)]
+        for f in (lib.bm_route_scored, lib.bm_moe_forward_routed, lib.bm_moe_forward_routed_quantized, lib.bm_add_adapters):
+            f.restype = i32
         for f in (lib.bm_quantize, lib.bm_add_rmsnorm, lib.bm_grouped_matmul, lib.bm_grouped_swiglu, lib.bm_moe_forward_quantized):
             f.restype = i32
         for f in (lib.bm_validate_tables, lib.bm_route_topk, lib.bm_buddy_remap, lib.bm_permute_by_expert,
@@ -291,3 +313,57 @@ def bm_moe_forward_quantized(desc: LayerDesc, x, x_q, x_scale, weights: Quantize
                                                    workspace.numel() * workspace.element_size(),
                                                    ctypes.byref(d) if d is not None else None,
                                                    _stream() if stream is None else stream), "bm_moe_forward_quantized")
+
+
+def bm_workspace_bytes_scored(desc: RouterDesc) -> int:
+    return int(load_library().bm_workspace_bytes_scored(ctypes.byref(desc)))
+
+
+def bm_route_scored(desc: RouterDesc, x, w_router, bias, balance, ids, w, workspace, stream: Optional[int] = None):
+    """Expert ids and weights by softmax or sigmoid scores, a balance bias and groups of experts."""
+    _check(load_library().bm_route_scored(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(bias), _ptr(balance), _ptr(ids),
+                                          _ptr(w), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                          _stream() if stream is None else stream), "bm_route_scored")
+
+
+def bm_moe_forward_routed(desc: LayerDesc, x, ids, w, weights: Weights, bitmap, table, y, workspace, dbg: Optional[dict] = None,
+                          stream: Optional[int] = None):
+    """bm_moe_forward on given expert ids and gate weights.  dbg as there."""
+    d = _debug_struct(dbg)
+    _check(load_library().bm_moe_forward_routed(ctypes.byref(desc), _ptr(x), _ptr(ids), _ptr(w), ctypes.byref(weights), _ptr(bitmap),
+                                                _ptr(table), _ptr(y), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                                ctypes.byref(d) if d is not None else None,
+                                                _stream() if stream is None else stream), "bm_moe_forward_routed")
+
+
+def bm_moe_forward_routed_quantized(desc: LayerDesc, x, x_q, x_scale, ids, w, weights: QuantizedWeights, bitmap, table, y, workspace,
+                                    dbg: Optional[dict] = None, stream: Optional[int] = None):
+    """bm_moe_forward_quantized on given expert ids and gate weights; x may be None when x_q and x_scale are given."""
+    d = _debug_struct(dbg)
+    _check(load_library().bm_moe_forward_routed_quantized(ctypes.byref(desc), _ptr(x), _ptr(x_q), _ptr(x_scale), _ptr(ids), _ptr(w),
+                                                          ctypes.byref(weights), _ptr(bitmap), _ptr(table), _ptr(y), _ptr(workspace),
+                                                          workspace.numel() * workspace.element_size(),
+                                                          ctypes.byref(d) if d is not None else None,
+                                                          _stream() if stream is None else stream), "bm_moe_forward_routed_quantized")
+
+
+def bm_workspace_bytes_adapters(desc: AdapterDesc) -> int:
+    return int(load_library().bm_workspace_bytes_adapters(ctypes.byref(desc)))
+
+
+def _rows_ptr(t, stride: int, width: int) -> Optional[int]:
+    """Address of a matrix [rows][width] whose rows lie `stride` values apart (0: width)."""
+    if t is None:
+        return None
+    assert t.dim() == 2 and t.size(1) == width and (t.size(0) < 2 or t.stride(0) == (stride or width)) and (width < 2 or t.stride(1) == 1), \
+        "rows must lie as the descriptor says"
+    return t.data_ptr()
+
+
+def bm_add_adapters(desc: AdapterDesc, x, adapter, a, b, ranks, scale, base, y, workspace, stream: Optional[int] = None):
+    """y = base + scale[s] * b[s] (a[s] x) with s = adapter[row]; x, base and y may be columns of wider matrices (desc's strides)."""
+    _check(load_library().bm_add_adapters(ctypes.byref(desc), _rows_ptr(x, desc.x_stride, desc.Kd), _ptr(adapter), _ptr(a), _ptr(b),
+                                          _ptr(ranks), _ptr(scale), _rows_ptr(base, desc.base_stride, desc.N),
+                                          _rows_ptr(y, desc.y_stride, desc.N), _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(),
+                                          _stream() if stream is None else stream), "bm_add_adapters")

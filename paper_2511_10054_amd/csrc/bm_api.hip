@@ -5,6 +5,8 @@
 #include "bm_dispatch_rules.h"
 #include "bm_device_shape.h"
 #include "bm_products.h"
+#include "bm_router.h"
+#include "bm_adapters.h"
 
 #include <atomic>
 #include <cstdio>
@@ -177,14 +179,14 @@ bool plan_layout(const bm_layer_desc *d, size_t bytes, Layout &L) {
 
 // Argument checks of the whole-layer entry points (everything but the workspace).
 int check_moe_args(const bm_layer_desc *desc, const void *x, const bm_weights *wt, const uint64_t *residency_bitmap,
-                   const int32_t *buddy_table, const void *y) {
+                   const int32_t *buddy_table, const void *y, bool given_routing) {
     int rc = check_desc(desc, true);
     if (rc) return rc;
     rc = check_remap_desc(desc);
     if (rc) return rc;
     if (desc->T == 0) return BM_OK;
     if (!x || !wt || !residency_bitmap || !y || (!buddy_table && desc->R > 0)) return BM_ERR_NULL;
-    if (!wt->w_router || !wt->w_gate || !wt->w_up || !wt->w_down) return BM_ERR_NULL;
+    if ((!wt->w_router && !given_routing) || !wt->w_gate || !wt->w_up || !wt->w_down) return BM_ERR_NULL;
     if (desc->n_shared > 0 && (!wt->ws_gate || !wt->ws_up || !wt->ws_down)) return BM_ERR_NULL;
     if ((desc->flags & BM_PSI_TOKEN) && !wt->buddy_q) return BM_ERR_NULL;
     return BM_OK;
@@ -267,12 +269,20 @@ struct FrontEnd {
     ScanParams sp;
     ScatterParams cp;
     bool fuse;
+    const int32_t *given_ids;     // the caller's routing: no router, fp.x and fp.wr are not read
+    const float *given_w;
+};
+
+// The caller's routing in place of the router's
+struct GivenRouting {
+    const int32_t *ids;           // [T][K], or null: the layer routes
+    const float *w;               // [T][K]
 };
 
 // logits_space: where the router's logits may go if they fit (nothing is held there before the projections)
 FrontEnd plan_front(const bm_layer_desc *desc, const void *x, const void *w_router, const float *router_bias, const float *buddy_q,
                     const uint64_t *residency_bitmap, const int32_t *buddy_table, void *ws, const Layout &L, float *logits_space,
-                    size_t logits_bytes) {
+                    size_t logits_bytes, const GivenRouting &given) {
     const int T = desc->T, K = desc->K, E = desc->E;
     FrontEnd f{};
     FrontParams &fp = f.fp;
@@ -285,7 +295,9 @@ FrontEnd plan_front(const bm_layer_desc *desc, const void *x, const void *w_rout
     fp.ids2 = at<int32_t>(ws, L.ids2);
     fp.tile_counts = at<int32_t>(ws, L.tile_counts);
     fp.tile_stats = at<int32_t>(ws, L.tile_stats);
-    f.fuse = front_can_fuse(T, desc->dtype, desc->flags);
+    f.given_ids = given.ids;
+    f.given_w = given.w;
+    f.fuse = !given.ids && front_can_fuse(T, desc->dtype, desc->flags);
     if (!f.fuse && front_wants_logits(fp, desc->dtype) && (size_t)T * E * 4 <= logits_bytes) fp.logits = logits_space;
     fp.tile_tokens = front_tile_tokens(T, desc->dtype, f.fuse);
 
@@ -318,20 +330,23 @@ int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, con
         fp.scan = sp;
         fp.scat = cp;
         err |= launch_front(fp, desc->dtype, st);
-    } else if (desc->flags & BM_GATE_DIST) {
+    } else if (f.given_ids || (desc->flags & BM_GATE_DIST)) {
         // the distribution gate needs every token's routing before the first substitution: route,
         // then substitute (each workgroup derives the batch's request set itself), then count
-        FrontParams rp = fp;
-        rp.bitmap = nullptr;
         const bool psi = (desc->flags & BM_PSI_TOKEN) != 0;
-        if (psi) rp.probs_out = at<float>(ws, L.probs);
-        err |= launch_front(rp, desc->dtype, st);
+        if (!f.given_ids) {
+            FrontParams rp = fp;
+            rp.bitmap = nullptr;
+            if (psi) rp.probs_out = at<float>(ws, L.probs);
+            err |= launch_front(rp, desc->dtype, st);
+        }
         RemapParams mp{};
         mp.T = T; mp.K = K; mp.E = E; mp.R = desc->R; mp.H = desc->H;
         mp.flags = desc->flags; mp.tau = fp.tau; mp.gamma = fp.gamma; mp.rho = fp.rho; mp.beta = fp.beta;
         mp.bitmap = fp.bitmap; mp.table = fp.table;
         mp.q = fp.q; mp.eta = fp.eta; mp.probs = psi ? at<float>(ws, L.probs) : nullptr;
-        mp.ids_in = fp.ids; mp.ids_out = fp.ids2; mp.w = fp.w; mp.stats = sp.stats;
+        mp.ids_in = f.given_ids ? f.given_ids : fp.ids; mp.w_in = f.given_w;
+        mp.ids_out = fp.ids2; mp.w = fp.w; mp.stats = sp.stats;
         err |= launch_remap(mp, st);
         if (!grouping_small((long long)T * K, E)) err |= launch_count(fp.ids2, T, K, E, fp.tile_tokens, fp.tile_counts, st);
         ScanParams sq = sp;
@@ -352,7 +367,7 @@ int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, con
 // The intermediate index arrays that a caller asked for
 int copy_debug(const bm_debug_out *dbg, const FrontEnd &f, hipStream_t st) {
     const size_t A = (size_t)f.fp.T * f.fp.K;
-    if (dbg->ids) copy_ints(f.fp.ids, dbg->ids, A, st);
+    if (dbg->ids) copy_ints(f.given_ids ? f.given_ids : f.fp.ids, dbg->ids, A, st);
     if (dbg->ids_remapped) copy_ints(f.fp.ids2, dbg->ids_remapped, A, st);
     if (dbg->w) copy_ints(f.fp.w, dbg->w, A, st);
     if (dbg->offsets) copy_ints(f.sp.offsets, dbg->offsets, (size_t)f.fp.E + 1, st);
@@ -457,6 +472,273 @@ ProductParams product_params(const bm_product_desc *d, const void *a, const floa
     p.offsets = offsets; p.E = p.n_groups = d->E;
     p.rows = d->rows; p.N = d->N; p.Kd = d->Kd;
     return p;
+}
+
+// The layer on checked arguments and a batch that is not empty
+int forward(const bm_layer_desc *desc, const void *x, const bm_weights *wt, const GivenRouting &given, const uint64_t *residency_bitmap,
+            const int32_t *buddy_table, void *y, void *workspace, size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
+    Layout L;
+    int rc = check_ws(desc, workspace, workspace_bytes, L);
+    if (rc) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    void *ws = workspace;
+    const int T = desc->T, K = desc->K, E = desc->E, G = E + desc->n_shared;
+    const bool bf16 = desc->dtype == BM_BF16;
+    int err = 0;
+    (void)hipGetLastError();   // errors left by earlier, unrelated HIP calls are not ours
+
+    hipEvent_t ev[5];
+    rc = stage_events(dbg, ev);
+    if (rc) return rc;
+    auto mark = [&](int i) { if (ev[i]) err |= (hipEventRecord(ev[i], st) != hipSuccess); };
+
+    // 1.-3. router, gates, substitution, grouping
+    mark(0);
+    // the logits borrow the space of h, which nothing holds before the gate/up projection
+    FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
+                             at<float>(ws, L.h), (size_t)L.rows_max * desc->F * (bf16 ? 2 : 4), given);
+    const FrontParams &fp = fe.fp;
+    ScanParams &sp = fe.sp;
+    const ScatterParams &cp = fe.cp;
+    const bool skinny = L.skinny;
+    const bool persistent = !skinny && bf16 && persistent_device();
+    const bool per_group = skinny || !bf16;              // decode and fp32 projections: one table entry per live group
+    const int mode_gu = per_group ? (1 << 30) : tile_mode(desc, false, persistent);
+    const int mode_dn = per_group ? (1 << 30) : tile_mode(desc, true, persistent);
+    // the plain table serves whichever projection runs a single tile height (both, unless one is mixed)
+    sp.BM = mode_gu != TILES_MIXED ? mode_gu : (mode_dn != TILES_MIXED ? mode_dn : 256);
+    if (mode_gu == TILES_MIXED || mode_dn == TILES_MIXED) {
+        sp.mixed = 1;
+        sp.mt_group_b = at<int32_t>(ws, L.mt_group_b); sp.mt_row0_b = at<int32_t>(ws, L.mt_row0_b);
+        sp.n_mtiles_b = at<int32_t>(ws, L.n_mtiles_b);
+        sp.mt_group_s = at<int32_t>(ws, L.mt_group_s); sp.mt_row0_s = at<int32_t>(ws, L.mt_row0_s);
+        sp.n_mtiles_s = at<int32_t>(ws, L.n_mtiles_s);
+    }
+    sp.largest_first = per_group ? 1 : 0;
+    err |= launch_front_end(desc, fe, ws, L, st);
+    mark(1);
+
+    // 4. gate/up projection + SwiGLU, 5. down projection
+    GemmParams gp{};
+    gp.a = x; gp.row_map = cp.row_token; gp.a_rows = T;
+    gp.b0 = wt->w_gate; gp.b1 = wt->w_up; gp.sb0 = wt->ws_gate; gp.sb1 = wt->ws_up;
+    gp.c = at<void>(ws, L.h);
+    gp.N = desc->F; gp.Kd = desc->d; gp.E = E; gp.n_groups = G; gp.max_mtiles = L.mtiles_max; gp.BM = sp.BM;
+    gp.mt_group = sp.mt_group; gp.mt_row0 = sp.mt_row0; gp.n_mtiles = sp.n_mtiles; gp.offsets = sp.offsets;
+    gp.cached_groups = cached_groups(desc);
+    GemmParams dp = gp;
+    auto use_mixed = [&](GemmParams &q) {
+        q.mixed = 1; q.BM = 256;
+        q.mt_group = sp.mt_group_b; q.mt_row0 = sp.mt_row0_b; q.n_mtiles = sp.n_mtiles_b;
+        q.mt_group_s = sp.mt_group_s; q.mt_row0_s = sp.mt_row0_s; q.n_mtiles_s = sp.n_mtiles_s;
+    };
+    if (mode_gu == TILES_MIXED) use_mixed(gp);
+    if (mode_dn == TILES_MIXED) use_mixed(dp);
+    dp.a = gp.c; dp.row_map = nullptr; dp.a_rows = L.rows_max;
+    dp.b0 = wt->w_down; dp.b1 = nullptr; dp.sb0 = wt->ws_down; dp.sb1 = nullptr;
+    dp.c = at<void>(ws, L.o);
+    dp.N = desc->d; dp.Kd = desc->F;
+    dp.splitk = L.has_splitk ? at<float>(ws, L.splitk) : nullptr;
+    dp.split_pieces = L.has_splitk ? at<int32_t>(ws, L.n_mtiles_s) + 4 : nullptr;
+    int ksplit = 1;
+    bool combined = false;                              // the down projection has written y itself
+    if (skinny) {
+        ksplit = L.ksplit;
+        SkinnyParams s1{};
+        s1.a = x; s1.row_map = cp.row_token;
+        s1.b0 = wt->w_gate; s1.b1 = wt->w_up; s1.sb0 = wt->ws_gate; s1.sb1 = wt->ws_up;
+        // packed copies are used only when every group of the layer has one
+        const bool pk_gu = wt->wp_gateup && (desc->n_shared == 0 || wt->wsp_gateup);
+        const bool pk_dn = wt->wp_down && (desc->n_shared == 0 || wt->wsp_down);
+        s1.pk = pk_gu ? wt->wp_gateup : nullptr; s1.spk = pk_gu ? wt->wsp_gateup : nullptr;
+        s1.c = gp.c; s1.N = desc->F; s1.Kd = desc->d; s1.E = E;
+        s1.max_groups = G < L.mtiles_max ? G : L.mtiles_max;
+        s1.ksplit = 1; s1.rows_max = L.rows_max; s1.max_rows_per_group = T * K;
+        // 128 rows per pass when big groups are likely (measured on the 8- and the 128-expert layer: the gate/up
+        // projection gains from 8 rows per expert on average, the down projection from 16)
+        s1.wide = (T > 64 && (long long)T * K >= 8ll * E) ? 1 : 0;
+        s1.mt_group = sp.mt_group; s1.n_mtiles = sp.n_mtiles; s1.offsets = sp.offsets;
+        SkinnyParams s2 = s1;
+        s2.a = gp.c; s2.row_map = nullptr;
+        s2.b0 = wt->w_down; s2.b1 = nullptr; s2.sb0 = wt->ws_down; s2.sb1 = nullptr;
+        s2.pk = pk_dn ? wt->wp_down : nullptr; s2.spk = pk_dn ? wt->wsp_down : nullptr;
+        s2.c = dp.c; s2.N = desc->d; s2.Kd = desc->F; s2.ksplit = ksplit;
+        s2.wide = (T > 64 && (long long)T * K >= 16ll * E) ? 1 : 0;
+        s1.narrow = narrow_gateup(desc) ? 1 : 0;                 // where the persistent kernel does not apply
+        s2.narrow = narrow_down(desc, L.compact) ? 1 : 0;
+        // small batches on a matrix as many 16-row blocks wide as the device has units: the down kernel
+        // aggregates its own results (null y: it writes them out for launch_combine below)
+        s2.y = y; s2.w = fp.w; s2.inv_perm = cp.inv_perm; s2.T = T; s2.K = K; s2.n_shared = desc->n_shared;
+        s2.y_f32 = (desc->flags & BM_Y_F32) ? 1 : 0;
+        combined = skinny_down_fuses_combine(s2);
+        if (!combined) s2.y = nullptr;
+        err |= launch_skinny_gateup_bf16(s1, st);
+        mark(2);
+        err |= launch_skinny_down_bf16(s2, st);
+    } else if (bf16) {
+        err |= launch_gateup_bf16(gp, st);
+        mark(2);
+        err |= launch_down_bf16(dp, st);
+    } else {
+        err |= launch_gateup_f32(gp, L.rows_max, T, st);
+        mark(2);
+        err |= launch_down_f32(dp, L.rows_max, T, st);
+    }
+    mark(3);
+
+    // 6. aggregation
+    CombineParams mp{};
+    mp.T = T; mp.d = desc->d; mp.K = K; mp.E = E; mp.n_shared = desc->n_shared;
+    mp.ksplit = ksplit; mp.slice_stride = (size_t)L.rows_max * desc->d;
+    mp.o = dp.c; mp.w = fp.w; mp.inv_perm = cp.inv_perm; mp.offsets = sp.offsets;
+    mp.y = y; mp.y_f32 = (!bf16 || (desc->flags & BM_Y_F32)) ? 1 : 0;
+    if (!combined) err |= launch_combine(mp, bf16 && !skinny, st);
+    mark(4);
+
+    if (dbg) err |= copy_debug(dbg, fe, st);
+    return err ? BM_ERR_HIP : BM_OK;
+}
+
+// Argument checks of the layer on 8-bit weights (everything but the workspace); routing null: the layer routes
+int check_quantized_args(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale, const bm_quantized_weights *wt,
+                         const uint64_t *residency_bitmap, const int32_t *buddy_table, const void *y, const GivenRouting *routing) {
+    int rc = check_quantized_desc(desc);
+    if (rc) return rc;
+    rc = check_remap_desc(desc);
+    if (rc) return rc;
+    if (routing && (desc->flags & BM_PSI_TOKEN)) return BM_ERR_SHAPE;     // needs the router's probabilities
+    if (desc->T == 0) return BM_OK;
+    // (the router alone reads x beside its 8-bit form)
+    if ((!x && !(routing && x_q)) || !wt || !residency_bitmap || !y || (!buddy_table && desc->R > 0) || !x_q != !x_scale) return BM_ERR_NULL;
+    if (routing && (!routing->ids || !routing->w)) return BM_ERR_NULL;
+    if (!routing && !wt->w_router) return BM_ERR_NULL;
+    if (!wt->w_gate || !wt->gate_scale || !wt->w_up || !wt->up_scale || !wt->w_down || !wt->down_scale) return BM_ERR_NULL;
+    if (desc->n_shared > 0 && (!wt->ws_gate || !wt->ws_gate_scale || !wt->ws_up || !wt->ws_up_scale || !wt->ws_down || !wt->ws_down_scale))
+        return BM_ERR_NULL;
+    if ((desc->flags & BM_PSI_TOKEN) && !wt->buddy_q) return BM_ERR_NULL;
+    if (off16(x) || off16(x_q) || off16(wt->w_gate) || off16(wt->w_up) || off16(wt->w_down) || off16(wt->ws_gate) ||
+        off16(wt->ws_up) || off16(wt->ws_down)) return BM_ERR_ALIGN;
+    return BM_OK;
+}
+
+int forward_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale, const bm_quantized_weights *wt,
+                      const GivenRouting &given, const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y, void *workspace,
+                      size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
+    const int T = desc->T, K = desc->K, E = desc->E, G = E + desc->n_shared;
+    const QuantizedLayout Q = make_quantized_layout(desc);
+    const Layout &L = Q.front;
+    void *ws = workspace;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) % ALIGN) || workspace_bytes < Q.total) return BM_ERR_WORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    hipEvent_t ev[5];
+    const int rc = stage_events(dbg, ev);
+    if (rc) return rc;
+    int err = 0;
+    (void)hipGetLastError();
+    auto mark = [&](int i) { if (ev[i]) err |= (hipEventRecord(ev[i], st) != hipSuccess); };
+
+    mark(0);
+    // the logits borrow the space of o, which nothing holds before the down projection
+    FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
+                             at<float>(ws, Q.o), (size_t)L.rows_max * desc->d * (Q.o_f32 ? 4 : 2), given);
+    fe.sp.BM = 1 << 30;                       // the products find their tiles from the offsets: the table is not read
+    uint8_t *const own_q = at<uint8_t>(ws, Q.xq);
+    float *const own_s = at<float>(ws, Q.xs);
+    const bool beside = !x_q && !given.ids && front_quantizes(fe.fp, fe.fuse);
+    if (beside) {
+        fe.fp.xq = own_q;
+        fe.fp.xs = own_s;
+    }
+    err |= launch_front_end(desc, fe, ws, L, st);
+    if (!x_q) {
+        if (!beside) err |= launch_quantize(x, false, own_q, own_s, 1, T, desc->d, false, st);
+        x_q = own_q;
+        x_scale = own_s;
+    }
+    mark(1);
+
+    ProductParams gp{};
+    gp.a = static_cast<const uint8_t *>(x_q); gp.a_scale = x_scale;
+    gp.row_map = fe.cp.row_token; gp.map_div = 1; gp.a_rows = T;
+    gp.b0 = static_cast<const uint8_t *>(wt->w_gate); gp.bs0 = wt->gate_scale;
+    gp.b1 = static_cast<const uint8_t *>(wt->w_up); gp.bs1 = wt->up_scale;
+    gp.sb0 = static_cast<const uint8_t *>(wt->ws_gate); gp.sbs0 = wt->ws_gate_scale;
+    gp.sb1 = static_cast<const uint8_t *>(wt->ws_up); gp.sbs1 = wt->ws_up_scale;
+    gp.offsets = fe.sp.offsets; gp.E = E; gp.n_groups = G;
+    gp.rows = L.rows_max; gp.N = desc->F; gp.Kd = desc->d;
+    gp.c = at<void>(ws, Q.h); gp.c_scale = at<float>(ws, Q.hs);
+    err |= launch_swiglu(gp, st);
+    mark(2);
+    ProductParams dp = gp;
+    dp.a = at<uint8_t>(ws, Q.h); dp.a_scale = at<float>(ws, Q.hs);
+    dp.row_map = nullptr; dp.a_rows = L.rows_max;
+    dp.b0 = static_cast<const uint8_t *>(wt->w_down); dp.bs0 = wt->down_scale;
+    dp.b1 = nullptr; dp.bs1 = nullptr; dp.sb1 = nullptr; dp.sbs1 = nullptr;
+    dp.sb0 = static_cast<const uint8_t *>(wt->ws_down); dp.sbs0 = wt->ws_down_scale;
+    dp.N = desc->d; dp.Kd = desc->F;
+    dp.c = at<void>(ws, Q.o); dp.c_scale = nullptr; dp.c_f32 = Q.o_f32;
+    err |= launch_product(dp, st);
+    mark(3);
+
+    CombineParams mp{};
+    mp.T = T; mp.d = desc->d; mp.K = K; mp.E = E; mp.n_shared = desc->n_shared;
+    mp.ksplit = 1; mp.slice_stride = 0;
+    mp.o = dp.c; mp.w = fe.fp.w; mp.inv_perm = fe.cp.inv_perm; mp.offsets = fe.sp.offsets;
+    mp.y = y; mp.y_f32 = (desc->flags & BM_Y_F32) ? 1 : 0;
+    err |= launch_combine(mp, !Q.o_f32, st);
+    mark(4);
+    if (dbg) err |= copy_debug(dbg, fe, st);
+    return err ? BM_ERR_HIP : BM_OK;
+}
+
+// ---- routing by scores, adapters ----
+
+int check_router(const bm_router_desc *d) {
+    if (!d) return BM_ERR_NULL;
+    if (d->dtype != BM_F32 && d->dtype != BM_BF16) return BM_ERR_DTYPE;
+    if (d->T < 0 || d->E <= 0 || d->K <= 0 || d->d <= 0 || d->d > MAX_ROUTER_D) return BM_ERR_SHAPE;
+    if (d->E > BM_MAX_E || d->K > BM_MAX_K || (long long)d->T * d->K > (1ll << 30)) return BM_ERR_SHAPE;
+    if (d->dtype == BM_BF16 && d->d % 32) return BM_ERR_SHAPE;
+    if (d->n_groups <= 0 || d->n_groups > MAX_ROUTER_GROUPS || d->E % d->n_groups) return BM_ERR_SHAPE;
+    const int per = d->E / d->n_groups;
+    if (d->keep_groups <= 0 || d->keep_groups > d->n_groups || d->K > d->keep_groups * per) return BM_ERR_SHAPE;
+    if ((d->group_top != 1 && d->group_top != 2) || d->group_top > per) return BM_ERR_SHAPE;
+    if (d->scoring != BM_SCORE_SOFTMAX && d->scoring != BM_SCORE_SIGMOID) return BM_ERR_SHAPE;
+    if (!(d->scale > -3.0e38f && d->scale < 3.0e38f)) return BM_ERR_SHAPE;
+    return BM_OK;
+}
+
+int check_adapters(const bm_adapter_desc *d) {
+    if (!d) return BM_ERR_NULL;
+    if ((d->dtype != BM_F32 && d->dtype != BM_BF16) || (d->y_dtype != BM_F32 && d->y_dtype != BM_BF16)) return BM_ERR_DTYPE;
+    if (d->rows < 0 || d->rows > MAX_ADAPTER_ROWS || d->Kd <= 0 || d->Kd > MAX_ADAPTER_WIDTH || d->N <= 0 || d->N > MAX_ADAPTER_WIDTH) return BM_ERR_SHAPE;
+    if (d->n <= 0 || d->n > BM_MAX_ADAPTERS || d->rank <= 0 || d->rank > BM_MAX_RANK) return BM_ERR_SHAPE;
+    if ((d->x_stride && d->x_stride < d->Kd) || (d->base_stride && d->base_stride < d->N) || (d->y_stride && d->y_stride < d->N)) return BM_ERR_SHAPE;
+    return BM_OK;
+}
+
+// Scratch of bm_add_adapters: the launch's plan, and its arrays at their places
+struct AdapterLayout {
+    AdapterParams p;
+    size_t order, tiles, n_tiles, u, total;
+};
+
+AdapterLayout make_adapter_layout(const bm_adapter_desc *d) {
+    AdapterLayout L{};
+    AdapterParams &p = L.p;
+    p.rows = d->rows; p.Kd = d->Kd; p.N = d->N; p.n = d->n; p.rank = d->rank;
+    p.x_stride = d->x_stride ? d->x_stride : d->Kd;
+    p.base_stride = d->base_stride ? d->base_stride : d->N;
+    p.y_stride = d->y_stride ? d->y_stride : d->N;
+    plan_adapters(p, d->dtype == BM_F32);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
+    L.order = take((size_t)p.u_rows * 4);
+    L.tiles = take((size_t)p.chunks * p.max_tiles * sizeof(AdapterTile));
+    L.n_tiles = take((size_t)p.chunks * 4);
+    L.u = take(adapter_u_rows(p) * p.width * 4);
+    L.total = off;
+    return L;
 }
 
 }  // namespace
@@ -650,7 +932,7 @@ int bm_permute_by_expert(const bm_layer_desc *desc, const int32_t *ids_remapped,
 int bm_moe_forward_static(const bm_layer_desc *desc, const void *x, const bm_weights *wt,
                           const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y,
                           const bm_debug_out *dbg, void *stream) {
-    int rc = check_moe_args(desc, x, wt, residency_bitmap, buddy_table, y);
+    int rc = check_moe_args(desc, x, wt, residency_bitmap, buddy_table, y, false);
     if (rc) return rc;
     if (desc->T == 0) return BM_OK;
     Layout L;
@@ -664,129 +946,20 @@ int bm_moe_forward_static(const bm_layer_desc *desc, const void *x, const bm_wei
 int bm_moe_forward(const bm_layer_desc *desc, const void *x, const bm_weights *wt,
                    const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y, void *workspace,
                    size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
-    int rc = check_moe_args(desc, x, wt, residency_bitmap, buddy_table, y);
+    const int rc = check_moe_args(desc, x, wt, residency_bitmap, buddy_table, y, false);
+    if (rc || desc->T == 0) return rc;
+    return forward(desc, x, wt, GivenRouting{}, residency_bitmap, buddy_table, y, workspace, workspace_bytes, dbg, stream);
+}
+
+int bm_moe_forward_routed(const bm_layer_desc *desc, const void *x, const int32_t *ids, const float *w, const bm_weights *wt,
+                          const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y, void *workspace,
+                          size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
+    const int rc = check_moe_args(desc, x, wt, residency_bitmap, buddy_table, y, true);
     if (rc) return rc;
+    if (desc->flags & BM_PSI_TOKEN) return BM_ERR_SHAPE;      // needs the router's probabilities
     if (desc->T == 0) return BM_OK;
-    Layout L;
-    rc = check_ws(desc, workspace, workspace_bytes, L);
-    if (rc) return rc;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    void *ws = workspace;
-    const int T = desc->T, K = desc->K, E = desc->E, G = E + desc->n_shared;
-    const bool bf16 = desc->dtype == BM_BF16;
-    int err = 0;
-    (void)hipGetLastError();   // errors left by earlier, unrelated HIP calls are not ours
-
-    hipEvent_t ev[5];
-    rc = stage_events(dbg, ev);
-    if (rc) return rc;
-    auto mark = [&](int i) { if (ev[i]) err |= (hipEventRecord(ev[i], st) != hipSuccess); };
-
-    // 1.-3. router, gates, substitution, grouping
-    mark(0);
-    // the logits borrow the space of h, which nothing holds before the gate/up projection
-    FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
-                             at<float>(ws, L.h), (size_t)L.rows_max * desc->F * (bf16 ? 2 : 4));
-    const FrontParams &fp = fe.fp;
-    ScanParams &sp = fe.sp;
-    const ScatterParams &cp = fe.cp;
-    const bool skinny = L.skinny;
-    const bool persistent = !skinny && bf16 && persistent_device();
-    const bool per_group = skinny || !bf16;              // decode and fp32 projections: one table entry per live group
-    const int mode_gu = per_group ? (1 << 30) : tile_mode(desc, false, persistent);
-    const int mode_dn = per_group ? (1 << 30) : tile_mode(desc, true, persistent);
-    // the plain table serves whichever projection runs a single tile height (both, unless one is mixed)
-    sp.BM = mode_gu != TILES_MIXED ? mode_gu : (mode_dn != TILES_MIXED ? mode_dn : 256);
-    if (mode_gu == TILES_MIXED || mode_dn == TILES_MIXED) {
-        sp.mixed = 1;
-        sp.mt_group_b = at<int32_t>(ws, L.mt_group_b); sp.mt_row0_b = at<int32_t>(ws, L.mt_row0_b);
-        sp.n_mtiles_b = at<int32_t>(ws, L.n_mtiles_b);
-        sp.mt_group_s = at<int32_t>(ws, L.mt_group_s); sp.mt_row0_s = at<int32_t>(ws, L.mt_row0_s);
-        sp.n_mtiles_s = at<int32_t>(ws, L.n_mtiles_s);
-    }
-    sp.largest_first = per_group ? 1 : 0;
-    err |= launch_front_end(desc, fe, ws, L, st);
-    mark(1);
-
-    // 4. gate/up projection + SwiGLU, 5. down projection
-    GemmParams gp{};
-    gp.a = x; gp.row_map = cp.row_token; gp.a_rows = T;
-    gp.b0 = wt->w_gate; gp.b1 = wt->w_up; gp.sb0 = wt->ws_gate; gp.sb1 = wt->ws_up;
-    gp.c = at<void>(ws, L.h);
-    gp.N = desc->F; gp.Kd = desc->d; gp.E = E; gp.n_groups = G; gp.max_mtiles = L.mtiles_max; gp.BM = sp.BM;
-    gp.mt_group = sp.mt_group; gp.mt_row0 = sp.mt_row0; gp.n_mtiles = sp.n_mtiles; gp.offsets = sp.offsets;
-    gp.cached_groups = cached_groups(desc);
-    GemmParams dp = gp;
-    auto use_mixed = [&](GemmParams &q) {
-        q.mixed = 1; q.BM = 256;
-        q.mt_group = sp.mt_group_b; q.mt_row0 = sp.mt_row0_b; q.n_mtiles = sp.n_mtiles_b;
-        q.mt_group_s = sp.mt_group_s; q.mt_row0_s = sp.mt_row0_s; q.n_mtiles_s = sp.n_mtiles_s;
-    };
-    if (mode_gu == TILES_MIXED) use_mixed(gp);
-    if (mode_dn == TILES_MIXED) use_mixed(dp);
-    dp.a = gp.c; dp.row_map = nullptr; dp.a_rows = L.rows_max;
-    dp.b0 = wt->w_down; dp.b1 = nullptr; dp.sb0 = wt->ws_down; dp.sb1 = nullptr;
-    dp.c = at<void>(ws, L.o);
-    dp.N = desc->d; dp.Kd = desc->F;
-    dp.splitk = L.has_splitk ? at<float>(ws, L.splitk) : nullptr;
-    dp.split_pieces = L.has_splitk ? at<int32_t>(ws, L.n_mtiles_s) + 4 : nullptr;
-    int ksplit = 1;
-    bool combined = false;                              // the down projection has written y itself
-    if (skinny) {
-        ksplit = L.ksplit;
-        SkinnyParams s1{};
-        s1.a = x; s1.row_map = cp.row_token;
-        s1.b0 = wt->w_gate; s1.b1 = wt->w_up; s1.sb0 = wt->ws_gate; s1.sb1 = wt->ws_up;
-        // packed copies are used only when every group of the layer has one
-        const bool pk_gu = wt->wp_gateup && (desc->n_shared == 0 || wt->wsp_gateup);
-        const bool pk_dn = wt->wp_down && (desc->n_shared == 0 || wt->wsp_down);
-        s1.pk = pk_gu ? wt->wp_gateup : nullptr; s1.spk = pk_gu ? wt->wsp_gateup : nullptr;
-        s1.c = gp.c; s1.N = desc->F; s1.Kd = desc->d; s1.E = E;
-        s1.max_groups = G < L.mtiles_max ? G : L.mtiles_max;
-        s1.ksplit = 1; s1.rows_max = L.rows_max; s1.max_rows_per_group = T * K;
-        // 128 rows per pass when big groups are likely (measured on the 8- and the 128-expert layer: the gate/up
-        // projection gains from 8 rows per expert on average, the down projection from 16)
-        s1.wide = (T > 64 && (long long)T * K >= 8ll * E) ? 1 : 0;
-        s1.mt_group = sp.mt_group; s1.n_mtiles = sp.n_mtiles; s1.offsets = sp.offsets;
-        SkinnyParams s2 = s1;
-        s2.a = gp.c; s2.row_map = nullptr;
-        s2.b0 = wt->w_down; s2.b1 = nullptr; s2.sb0 = wt->ws_down; s2.sb1 = nullptr;
-        s2.pk = pk_dn ? wt->wp_down : nullptr; s2.spk = pk_dn ? wt->wsp_down : nullptr;
-        s2.c = dp.c; s2.N = desc->d; s2.Kd = desc->F; s2.ksplit = ksplit;
-        s2.wide = (T > 64 && (long long)T * K >= 16ll * E) ? 1 : 0;
-        s1.narrow = narrow_gateup(desc) ? 1 : 0;                 // where the persistent kernel does not apply
-        s2.narrow = narrow_down(desc, L.compact) ? 1 : 0;
-        // small batches on a matrix as many 16-row blocks wide as the device has units: the down kernel
-        // aggregates its own results (null y: it writes them out for launch_combine below)
-        s2.y = y; s2.w = fp.w; s2.inv_perm = cp.inv_perm; s2.T = T; s2.K = K; s2.n_shared = desc->n_shared;
-        s2.y_f32 = (desc->flags & BM_Y_F32) ? 1 : 0;
-        combined = skinny_down_fuses_combine(s2);
-        if (!combined) s2.y = nullptr;
-        err |= launch_skinny_gateup_bf16(s1, st);
-        mark(2);
-        err |= launch_skinny_down_bf16(s2, st);
-    } else if (bf16) {
-        err |= launch_gateup_bf16(gp, st);
-        mark(2);
-        err |= launch_down_bf16(dp, st);
-    } else {
-        err |= launch_gateup_f32(gp, L.rows_max, T, st);
-        mark(2);
-        err |= launch_down_f32(dp, L.rows_max, T, st);
-    }
-    mark(3);
-
-    // 6. aggregation
-    CombineParams mp{};
-    mp.T = T; mp.d = desc->d; mp.K = K; mp.E = E; mp.n_shared = desc->n_shared;
-    mp.ksplit = ksplit; mp.slice_stride = (size_t)L.rows_max * desc->d;
-    mp.o = dp.c; mp.w = fp.w; mp.inv_perm = cp.inv_perm; mp.offsets = sp.offsets;
-    mp.y = y; mp.y_f32 = (!bf16 || (desc->flags & BM_Y_F32)) ? 1 : 0;
-    if (!combined) err |= launch_combine(mp, bf16 && !skinny, st);
-    mark(4);
-
-    if (dbg) err |= copy_debug(dbg, fe, st);
-    return err ? BM_ERR_HIP : BM_OK;
+    if (!ids || !w) return BM_ERR_NULL;
+    return forward(desc, x, wt, GivenRouting{ids, w}, residency_bitmap, buddy_table, y, workspace, workspace_bytes, dbg, stream);
 }
 
 int bm_quantize(const bm_quantize_desc *d, const void *src, void *q, float *scale, void *stream) {
@@ -857,83 +1030,70 @@ size_t bm_workspace_bytes_quantized(const bm_layer_desc *desc) {
 int bm_moe_forward_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale,
                              const bm_quantized_weights *wt, const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y,
                              void *workspace, size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
-    int rc = check_quantized_desc(desc);
-    if (rc) return rc;
-    rc = check_remap_desc(desc);
-    if (rc) return rc;
-    const int T = desc->T, K = desc->K, E = desc->E, G = E + desc->n_shared;
-    if (T == 0) return BM_OK;
-    if (!x || !wt || !residency_bitmap || !y || (!buddy_table && desc->R > 0) || !x_q != !x_scale) return BM_ERR_NULL;
-    if (!wt->w_router || !wt->w_gate || !wt->gate_scale || !wt->w_up || !wt->up_scale || !wt->w_down || !wt->down_scale) return BM_ERR_NULL;
-    if (desc->n_shared > 0 && (!wt->ws_gate || !wt->ws_gate_scale || !wt->ws_up || !wt->ws_up_scale || !wt->ws_down || !wt->ws_down_scale))
-        return BM_ERR_NULL;
-    if ((desc->flags & BM_PSI_TOKEN) && !wt->buddy_q) return BM_ERR_NULL;
-    if (off16(x) || off16(x_q) || off16(wt->w_gate) || off16(wt->w_up) || off16(wt->w_down) || off16(wt->ws_gate) ||
-        off16(wt->ws_up) || off16(wt->ws_down)) return BM_ERR_ALIGN;
-    const QuantizedLayout Q = make_quantized_layout(desc);
-    const Layout &L = Q.front;
-    void *ws = workspace;
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) % ALIGN) || workspace_bytes < Q.total) return BM_ERR_WORKSPACE;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    hipEvent_t ev[5];
-    rc = stage_events(dbg, ev);
-    if (rc) return rc;
-    int err = 0;
+    const int rc = check_quantized_args(desc, x, x_q, x_scale, wt, residency_bitmap, buddy_table, y, nullptr);
+    if (rc || desc->T == 0) return rc;
+    return forward_quantized(desc, x, x_q, x_scale, wt, GivenRouting{}, residency_bitmap, buddy_table, y, workspace, workspace_bytes, dbg, stream);
+}
+
+int bm_moe_forward_routed_quantized(const bm_layer_desc *desc, const void *x, const void *x_q, const float *x_scale,
+                                    const int32_t *ids, const float *w, const bm_quantized_weights *wt,
+                                    const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y, void *workspace,
+                                    size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
+    const GivenRouting given{ids, w};
+    const int rc = check_quantized_args(desc, x, x_q, x_scale, wt, residency_bitmap, buddy_table, y, &given);
+    if (rc || desc->T == 0) return rc;
+    return forward_quantized(desc, x, x_q, x_scale, wt, given, residency_bitmap, buddy_table, y, workspace, workspace_bytes, dbg, stream);
+}
+
+size_t bm_workspace_bytes_scored(const bm_router_desc *desc) {
+    if (check_router(desc) != BM_OK) return 0;
+    return align_up(router_scratch_bytes(desc->T, desc->d, desc->E, desc->dtype == BM_F32));
+}
+
+int bm_route_scored(const bm_router_desc *desc, const void *x, const void *w_router, const float *bias, const float *balance,
+                    int32_t *ids, float *w, void *workspace, size_t workspace_bytes, void *stream) {
+    const int rc = check_router(desc);
+    if (rc || desc->T == 0) return rc;
+    if (!x || !w_router || !ids || !w) return BM_ERR_NULL;
+    const bool f32 = desc->dtype == BM_F32;
+    if (!f32 && (off16(x) || off16(w_router))) return BM_ERR_ALIGN;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % ALIGN) || workspace_bytes < bm_workspace_bytes_scored(desc)) return BM_ERR_WORKSPACE;
     (void)hipGetLastError();
-    auto mark = [&](int i) { if (ev[i]) err |= (hipEventRecord(ev[i], st) != hipSuccess); };
+    RouterParams p{};
+    p.x = x; p.w = w_router; p.bias = bias; p.balance = balance;
+    p.logits = static_cast<float *>(workspace);
+    p.T = desc->T; p.d = desc->d; p.E = desc->E; p.K = desc->K;
+    p.n_groups = desc->n_groups; p.keep_groups = desc->keep_groups; p.group_top = desc->group_top;
+    p.sigmoid = desc->scoring == BM_SCORE_SIGMOID;
+    p.renorm = (desc->flags & BM_RENORM_TOPK) != 0;
+    p.scale = desc->scale;
+    p.ids = ids; p.weights = w;
+    return launch_route_scored(p, f32, static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
+}
 
-    mark(0);
-    // the logits borrow the space of o, which nothing holds before the down projection
-    FrontEnd fe = plan_front(desc, x, wt->w_router, wt->router_bias, wt->buddy_q, residency_bitmap, buddy_table, ws, L,
-                             at<float>(ws, Q.o), (size_t)L.rows_max * desc->d * (Q.o_f32 ? 4 : 2));
-    fe.sp.BM = 1 << 30;                       // the products find their tiles from the offsets: the table is not read
-    uint8_t *const own_q = at<uint8_t>(ws, Q.xq);
-    float *const own_s = at<float>(ws, Q.xs);
-    const bool beside = !x_q && front_quantizes(fe.fp, fe.fuse);
-    if (beside) {
-        fe.fp.xq = own_q;
-        fe.fp.xs = own_s;
-    }
-    err |= launch_front_end(desc, fe, ws, L, st);
-    if (!x_q) {
-        if (!beside) err |= launch_quantize(x, false, own_q, own_s, 1, T, desc->d, false, st);
-        x_q = own_q;
-        x_scale = own_s;
-    }
-    mark(1);
+size_t bm_workspace_bytes_adapters(const bm_adapter_desc *desc) {
+    if (check_adapters(desc) != BM_OK) return 0;
+    return make_adapter_layout(desc).total;
+}
 
-    ProductParams gp{};
-    gp.a = static_cast<const uint8_t *>(x_q); gp.a_scale = x_scale;
-    gp.row_map = fe.cp.row_token; gp.map_div = 1; gp.a_rows = T;
-    gp.b0 = static_cast<const uint8_t *>(wt->w_gate); gp.bs0 = wt->gate_scale;
-    gp.b1 = static_cast<const uint8_t *>(wt->w_up); gp.bs1 = wt->up_scale;
-    gp.sb0 = static_cast<const uint8_t *>(wt->ws_gate); gp.sbs0 = wt->ws_gate_scale;
-    gp.sb1 = static_cast<const uint8_t *>(wt->ws_up); gp.sbs1 = wt->ws_up_scale;
-    gp.offsets = fe.sp.offsets; gp.E = E; gp.n_groups = G;
-    gp.rows = L.rows_max; gp.N = desc->F; gp.Kd = desc->d;
-    gp.c = at<void>(ws, Q.h); gp.c_scale = at<float>(ws, Q.hs);
-    err |= launch_swiglu(gp, st);
-    mark(2);
-    ProductParams dp = gp;
-    dp.a = at<uint8_t>(ws, Q.h); dp.a_scale = at<float>(ws, Q.hs);
-    dp.row_map = nullptr; dp.a_rows = L.rows_max;
-    dp.b0 = static_cast<const uint8_t *>(wt->w_down); dp.bs0 = wt->down_scale;
-    dp.b1 = nullptr; dp.bs1 = nullptr; dp.sb1 = nullptr; dp.sbs1 = nullptr;
-    dp.sb0 = static_cast<const uint8_t *>(wt->ws_down); dp.sbs0 = wt->ws_down_scale;
-    dp.N = desc->d; dp.Kd = desc->F;
-    dp.c = at<void>(ws, Q.o); dp.c_scale = nullptr; dp.c_f32 = Q.o_f32;
-    err |= launch_product(dp, st);
-    mark(3);
-
-    CombineParams mp{};
-    mp.T = T; mp.d = desc->d; mp.K = K; mp.E = E; mp.n_shared = desc->n_shared;
-    mp.ksplit = 1; mp.slice_stride = 0;
-    mp.o = dp.c; mp.w = fe.fp.w; mp.inv_perm = fe.cp.inv_perm; mp.offsets = fe.sp.offsets;
-    mp.y = y; mp.y_f32 = (desc->flags & BM_Y_F32) ? 1 : 0;
-    err |= launch_combine(mp, !Q.o_f32, st);
-    mark(4);
-    if (dbg) err |= copy_debug(dbg, fe, st);
-    return err ? BM_ERR_HIP : BM_OK;
+int bm_add_adapters(const bm_adapter_desc *desc, const void *x, const int32_t *adapter, const void *a, const void *b,
+                    const int32_t *ranks, const float *scale, const void *base, void *y, void *workspace, size_t workspace_bytes,
+                    void *stream) {
+    const int rc = check_adapters(desc);
+    if (rc || desc->rows == 0) return rc;
+    if (!x || !adapter || !a || !b || !base || !y) return BM_ERR_NULL;
+    AdapterLayout L = make_adapter_layout(desc);
+    AdapterParams &p = L.p;
+    if (base == y && p.base_stride != p.y_stride) return BM_ERR_SHAPE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % ALIGN) || workspace_bytes < L.total) return BM_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    p.x = x; p.adapter = adapter; p.a = a; p.b = b; p.ranks = ranks; p.scale = scale;
+    p.base = base; p.y = y; p.in_place = base == y;
+    p.order = at<int32_t>(workspace, L.order);
+    p.tiles = at<AdapterTile>(workspace, L.tiles);
+    p.n_tiles = at<int32_t>(workspace, L.n_tiles);
+    p.u = at<float>(workspace, L.u);
+    return launch_adapters(p, desc->dtype == BM_F32, desc->y_dtype == BM_F32, static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
 }
 
 }  // extern "C"

@@ -1416,6 +1416,10 @@ __global__ void __launch_bounds__(1024) remap_kernel(RemapParams p) {
             for (int idx = tid; idx < n; idx += blockDim.x) s_ids[idx] = in[idx];
             __syncthreads();
         }
+        if (p.w_in != nullptr) {
+            for (int idx = tid; idx < n; idx += blockDim.x) p.w[(size_t)t0 * p.K + idx] = p.w_in[(size_t)t0 * p.K + idx];
+            __syncthreads();
+        }
         PsiSource psi{};
         if (p.flags & BM_PSI_TOKEN) { psi.q = p.q; psi.eta = p.eta; psi.stride = p.E; psi.probs = p.probs + (size_t)t0 * p.E; }
         remap_tile<W, KC>(ntok, p.K, p.E, p.R, p.flags, p.tau, p.gamma, p.rho, resident, accept, s_table, s_ids,

@@ -21,6 +21,7 @@ struct RemapParams {
     const int32_t *ids_in;
     int32_t *ids_out;
     float *w;
+    const float *w_in;      // [T][K] copied to w first, or null
     int32_t *stats;         // 6 ints or null
 };
 

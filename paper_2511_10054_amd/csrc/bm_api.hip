@@ -1047,7 +1047,7 @@ int bm_moe_forward_routed_quantized(const bm_layer_desc *desc, const void *x, co
 
 size_t bm_workspace_bytes_scored(const bm_router_desc *desc) {
     if (check_router(desc) != BM_OK) return 0;
-    return align_up(router_scratch_bytes(desc->T, desc->d, desc->E, desc->dtype == BM_F32));
+    return align_up(router_scratch_bytes(desc->T, desc->E));
 }
 
 int bm_route_scored(const bm_router_desc *desc, const void *x, const void *w_router, const float *bias, const float *balance,

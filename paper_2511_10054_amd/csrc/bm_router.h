@@ -21,7 +21,7 @@ struct RouterParams {
     float *weights;               // [T][K]
 };
 
-size_t router_scratch_bytes(int T, int d, int E, bool f32);
+size_t router_scratch_bytes(int T, int E);
 int launch_route_scored(const RouterParams &p, bool f32, hipStream_t st);
 
 }  // namespace bm

@@ -93,33 +93,59 @@ __global__ void __launch_bounds__(64) router_small_kernel(RouterParams p) {
 }
 
 // ---------------------------------------------------------------------------
-// The product for many tokens: 128 tokens x EB experts and a quarter (two parts) of the reduction a workgroup.  Whole lines of both
-// operands go through registers into one of two LDS stages, a row's 16-byte pieces turned by its number against bank conflicts; the
-// next line is on its way while one is multiplied.
+// The product for many tokens: 128 tokens x EB experts and a quarter (two parts) of the reduction a workgroup of eight waves.
+// Whole lines of both operands go straight into a ring of S LDS stages (8 rows an instruction); row r's 16-byte piece c lies at
+// slot c ^ (r & 7), by the choice of the piece that a lane fetches: conflict-free reads.  One wait and one barrier a line: its
+// stage has landed for every wave, and everybody is done with the stage that takes the next loads.
+// Bound by the way from the second-level caches into LDS, whose rate is what is in flight over the time that a load takes: all
+// experts in one workgroup, and as many stages as LDS holds.
 // ---------------------------------------------------------------------------
-constexpr int TILE_TOKENS = 128;
+#define BM_LDS __attribute__((address_space(3)))
+constexpr int TILE_TOKENS = 128, TILE_WAVES = 8;
+
+template <int EB>
+struct RouterTile {
+    static constexpr int WN = EB == 256 ? 4 : EB >= 64 ? 2 : 1, WM = TILE_WAVES / WN;     // waves along experts and tokens
+    static constexpr int TM = TILE_TOKENS / WM / 16, TN = EB / WN / 16;                  // 16 x 16 blocks of a wave
+    static constexpr int BLOCKS = (TILE_TOKENS + EB) / 8;                                // of 8 rows
+    static constexpr int LOADS = (BLOCKS + TILE_WAVES - 1) / TILE_WAVES;                 // a wave and stage
+    static constexpr int STAGES = EB == 128 ? 4 : 3, STAGE = BLOCKS * 64;                // 16-byte pieces of a stage
+    static constexpr size_t LDS = (size_t)STAGES * STAGE * 16;
+};
 
 template <typename L, int EB>
-__global__ void __launch_bounds__(256, 2) router_tile_kernel(RouterParams p) {
-    constexpr int WN = EB == 128 ? 2 : 1, WM = 4 / WN;                    // waves along experts and tokens
-    constexpr int TM = TILE_TOKENS / WM / 16, TN = EB / WN / 16;          // 16 x 16 blocks of a wave
-    constexpr int ROWS = TILE_TOKENS + EB, PER = ROWS / 32;               // rows of a stage, pieces a thread moves
-    __shared__ u32x4 stage[2][ROWS * 8];
-    const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, r16 = lane & 15, kq = lane >> 4;
-    const int e0 = blockIdx.x * EB, t0 = blockIdx.y * TILE_TOKENS, part = blockIdx.z * 2;
+__global__ void __launch_bounds__(TILE_WAVES * 64, 2) router_tile_kernel(RouterParams p) {
+    using R = RouterTile<EB>;
+    constexpr int S = R::STAGES, TM = R::TM, TN = R::TN;
+    extern __shared__ u32x4 smem[];
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, kq = lane >> 4;
+    // workgroups go round the eight dies: two dies a quarter (its columns of the router's matrix stay in their second-level caches),
+    // and a tile's tokens with all of the experts one after the other on one die
+    const int die = blockIdx.x & 7, turn = blockIdx.x >> 3, quarter = die & 3, part = quarter * 2;
+    const int expert_tiles = (p.E + EB - 1) / EB;
+    const int e0 = turn % expert_tiles * EB, t0 = (turn / expert_tiles * 2 + (die >> 2)) * TILE_TOKENS;
+    if (t0 >= p.T) return;
     const int bytes = p.d * (128 / L::VALUES), lines = (bytes + 127) >> 7;
     const int begin = part * lines / PARTS, middle = (part + 1) * lines / PARTS, end = (part + 2) * lines / PARTS;
-    const int row0 = tid >> 3, at0 = (tid & 7) * 16;
-    const char *from[PER];
+    const char *from[R::LOADS];
+    int to[R::LOADS], piece_at;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int row = row0 + 32 * j;
+    for (int j = 0; j < R::LOADS; ++j) {
+        int block = wave + TILE_WAVES * j;
+        if (block >= R::BLOCKS) block = wave % R::BLOCKS;                // (a repeated load of what is there)
+        const int row = block * 8 + (lane >> 3);
         from[j] = row < TILE_TOKENS ? static_cast<const char *>(p.x) + (size_t)min(t0 + row, p.T - 1) * bytes
                                     : static_cast<const char *>(p.w) + (size_t)min(e0 + row - TILE_TOKENS, p.E - 1) * bytes;
+        to[j] = block * 64;
     }
-    const int slot = row0 * 8 + ((tid & 7) ^ (row0 & 7));                 // (32 rows on, the same turn)
-    const int m0 = wave % WM * (TM * 16), n0 = TILE_TOKENS + wave / WM * (TN * 16);
-    u32x4 next[PER];
+    piece_at = ((lane & 7) ^ (lane >> 3)) * 16;
+    auto load = [&](int l, int slot) {
+        const int at = min(l, end - 1) * 128 + piece_at, within = at < bytes ? at : 0;   // (behind a row's end: cleared when read)
+#pragma unroll
+        for (int j = 0; j < R::LOADS; ++j)
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(from[j] + within), (BM_LDS void *)(smem + slot * R::STAGE + to[j]), 16, 0, 0);
+    };
+    const int m0 = wave % R::WM * (TM * 16), n0 = TILE_TOKENS + wave / R::WM * (TN * 16);
     f32x4 acc[TM][TN], first[TM][TN];
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -127,44 +153,47 @@ __global__ void __launch_bounds__(256, 2) router_tile_kernel(RouterParams p) {
         for (int j = 0; j < TN; ++j) acc[i][j] = first[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (begin < end) {
 #pragma unroll
-        for (int j = 0; j < PER; ++j) next[j] = piece<true>(from[j], begin * 128 + at0, bytes);
+        for (int i = 0; i < S - 1; ++i) load(begin + i, i);
+        int now = 0, free = S - 1;
+        for (int l = begin; l < end; ++l) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
+            load(l + S - 1, free);
+            const u32x4 *st = smem + now * R::STAGE;
+            if (l == middle)
 #pragma unroll
-        for (int j = 0; j < PER; ++j) stage[0][slot + 256 * j] = next[j];
-    }
-    __syncthreads();
-    for (int l = begin; l < end; ++l) {
-        const u32x4 *now = stage[(l - begin) & 1];
-        const bool more = l + 1 < end;
-        if (more)
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < PER; ++j) next[j] = piece<true>(from[j], (l + 1) * 128 + at0, bytes);
-        if (l == middle)
+                    for (int j = 0; j < TN; ++j) {
+                        first[i][j] = acc[i][j];
+                        acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    }
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int h = 0; h < 2; ++h) {
+                u32x4 a[TM], b[TN];
+                const int c = (h * 4 + kq) ^ (r16 & 7);
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    first[i][j] = acc[i][j];
-                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < TM; ++i) a[i] = st[(m0 + i * 16 + r16) * 8 + c];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) b[j] = st[(n0 + j * 16 + r16) * 8 + c];
+                if (l * 128 + 128 > bytes) {                             // the row ends in this line
+                    const bool in = l * 128 + (h * 4 + kq) * 16 < bytes;
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) a[i] = in ? a[i] : u32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) b[j] = in ? b[j] : u32x4{0, 0, 0, 0};
                 }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            u32x4 a[TM], b[TN];
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int i = 0; i < TM; ++i) a[i] = now[(m0 + i * 16 + r16) * 8 + ((h * 4 + kq) ^ (r16 & 7))];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) b[j] = now[(n0 + j * 16 + r16) * 8 + ((h * 4 + kq) ^ (r16 & 7))];
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int j = 0; j < TN; ++j) acc[i][j] = L::mac(a[i], b[j], acc[i][j]);
+                    for (int j = 0; j < TN; ++j) acc[i][j] = L::mac(a[i], b[j], acc[i][j]);
+            }
+            free = now;
+            now = now + 1 == S ? 0 : now + 1;
         }
-        if (more)
-#pragma unroll
-            for (int j = 0; j < PER; ++j) stage[(l + 1 - begin) & 1][slot + 256 * j] = next[j];
-        __syncthreads();
+        asm volatile("s_waitcnt vmcnt(0)" : : : "memory");               // the last loads are through before the workgroup ends
     }
-    // (a first part without lines: its sum is the zero in acc, which the second has started from)
-    float *out = p.logits + (size_t)blockIdx.z * p.T * p.E;
+    // (a first part without lines: its sum is the zero that acc starts from)
+    float *out = p.logits + (size_t)quarter * p.T * p.E;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int e = e0 + n0 - TILE_TOKENS + j * 16 + r16;
@@ -394,12 +423,18 @@ void launch_select(const RouterParams &p, hipStream_t st) {
     else hipLaunchKernelGGL((select_kernel<4, N>), grid, block, 0, st, p);
 }
 
+template <typename L, int EB>
+void launch_tile(const RouterParams &p, hipStream_t st) {
+    const int pairs = (p.T + 2 * TILE_TOKENS - 1) / (2 * TILE_TOKENS);     // of token tiles: one for each half of the dies
+    hipLaunchKernelGGL((router_tile_kernel<L, EB>), dim3((p.E + EB - 1) / EB * pairs * 8), dim3(TILE_WAVES * 64), RouterTile<EB>::LDS, st, p);
+}
+
 template <typename L>
 void launch_tiles(const RouterParams &p, hipStream_t st) {
-    const int tiles = (p.T + TILE_TOKENS - 1) / TILE_TOKENS;
-    if (p.E <= 32) hipLaunchKernelGGL((router_tile_kernel<L, 32>), dim3((p.E + 31) / 32, tiles, PARTS / 2), dim3(256), 0, st, p);
-    else if (p.E <= 64) hipLaunchKernelGGL((router_tile_kernel<L, 64>), dim3((p.E + 63) / 64, tiles, PARTS / 2), dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((router_tile_kernel<L, 128>), dim3((p.E + 127) / 128, tiles, PARTS / 2), dim3(256), 0, st, p);
+    if (p.E <= 32) launch_tile<L, 32>(p, st);
+    else if (p.E <= 64) launch_tile<L, 64>(p, st);
+    else if (p.E <= 128) launch_tile<L, 128>(p, st);
+    else launch_tile<L, 256>(p, st);
 }
 
 constexpr int CHUNK = 16384;             // tokens whose logits lie in the scratch at once

@@ -15,6 +15,7 @@ struct RouterParams {
     float *logits;                // [parts][T][E] scratch, without the bias
     int T, d, E, K;
     int n_groups, keep_groups, group_top;
+    int per_group, lanes_per_group;      // set by the launch
     bool sigmoid, renorm;
     float scale;
     int32_t *ids;                 // [T][K]

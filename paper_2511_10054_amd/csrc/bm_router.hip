@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(64) router_small_kernel(RouterParams p) {
 }
 
 // ---------------------------------------------------------------------------
-// The product for many tokens: 128 tokens x EB experts and a quarter (two parts) of the reduction a workgroup of eight waves.
+// The product for many tokens: 128 tokens x EB experts and TAKE of the eight parts of the reduction a workgroup of eight waves.
 // Whole lines of both operands go straight into a ring of S LDS stages (8 rows an instruction); row r's 16-byte piece c lies at
 // slot c ^ (r & 7), by the choice of the piece that a lane fetches: conflict-free reads.  One wait and one barrier a line: its
 // stage has landed for every wave, and everybody is done with the stage that takes the next loads.
@@ -113,20 +113,21 @@ struct RouterTile {
     static constexpr size_t LDS = (size_t)STAGES * STAGE * 16;
 };
 
-template <typename L, int EB>
+template <typename L, int EB, int TAKE>
 __global__ void __launch_bounds__(TILE_WAVES * 64, 2) router_tile_kernel(RouterParams p) {
     using R = RouterTile<EB>;
     constexpr int S = R::STAGES, TM = R::TM, TN = R::TN;
     extern __shared__ u32x4 smem[];
     const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, kq = lane >> 4;
-    // workgroups go round the eight dies: two dies a quarter (its columns of the router's matrix stay in their second-level caches),
-    // and a tile's tokens with all of the experts one after the other on one die
-    const int die = blockIdx.x & 7, turn = blockIdx.x >> 3, quarter = die & 3, part = quarter * 2;
+    // Workgroups go round the eight dies: a die (two dies) for an eighth (a quarter) of the reduction, whose columns of the router's
+    // matrix stay in its second-level cache, and a tile's tokens with all of the experts one after the other on one die
+    constexpr int SLICES = PARTS / TAKE;
+    const int die = blockIdx.x & 7, turn = blockIdx.x >> 3, slice = die % SLICES, part = slice * TAKE;
     const int expert_tiles = (p.E + EB - 1) / EB;
-    const int e0 = turn % expert_tiles * EB, t0 = (turn / expert_tiles * 2 + (die >> 2)) * TILE_TOKENS;
+    const int e0 = turn % expert_tiles * EB, t0 = (turn / expert_tiles * TAKE + die / SLICES) * TILE_TOKENS;
     if (t0 >= p.T) return;
     const int bytes = p.d * (128 / L::VALUES), lines = (bytes + 127) >> 7;
-    const int begin = part * lines / PARTS, middle = (part + 1) * lines / PARTS, end = (part + 2) * lines / PARTS;
+    const int begin = part * lines / PARTS, middle = (part + 1) * lines / PARTS, end = (part + TAKE) * lines / PARTS;
     const char *from[R::LOADS];
     int to[R::LOADS], piece_at;
 #pragma unroll
@@ -151,49 +152,69 @@ __global__ void __launch_bounds__(TILE_WAVES * 64, 2) router_tile_kernel(RouterP
     for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = first[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Fragments of the two halves of a line: those of one are read while the other's are multiplied.  Between the halves stand a wait and
+    // a barrier: the next line has landed for every wave, and this one's reads are done - its stage takes new loads.
+    u32x4 a[2][TM], b[2][TN];
+    int now = 0;
+    auto read = [&](int h) {
+        const u32x4 *st = smem + now * R::STAGE;
+        const int c = (h * 4 + kq) ^ (r16 & 7);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) a[h][i] = st[(m0 + i * 16 + r16) * 8 + c];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[h][j] = st[(n0 + j * 16 + r16) * 8 + c];
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = L::mac(a[h][i], b[h][j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto line = [&](int l) {
+        read(1);
+        multiply(0);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
+        load(l + S, now);
+        now = now + 1 == S ? 0 : now + 1;
+        read(0);
+        multiply(1);
+    };
     if (begin < end) {
 #pragma unroll
-        for (int i = 0; i < S - 1; ++i) load(begin + i, i);
-        int now = 0, free = S - 1;
-        for (int l = begin; l < end; ++l) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
-            load(l + S - 1, free);
-            const u32x4 *st = smem + now * R::STAGE;
-            if (l == middle)
+        for (int i = 0; i < S; ++i) load(begin + i, i);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((S - 1) * R::LOADS) : "memory");
+        read(0);
+        int l = begin;
+        for (; l < min(middle, end - 1); ++l) line(l);
+        if (TAKE == 2 && middle < end) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        first[i][j] = acc[i][j];
-                        acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    }
+                for (int j = 0; j < TN; ++j) {
+                    first[i][j] = acc[i][j];
+                    acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+            for (; l < end - 1; ++l) line(l);
+        }
+        read(1);
+        if (l * 128 + 128 > bytes) {                                     // the row ends in the last line
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                u32x4 a[TM], b[TN];
-                const int c = (h * 4 + kq) ^ (r16 & 7);
+                const bool in = l * 128 + (h * 4 + kq) * 16 < bytes;
 #pragma unroll
-                for (int i = 0; i < TM; ++i) a[i] = st[(m0 + i * 16 + r16) * 8 + c];
+                for (int i = 0; i < TM; ++i) a[h][i] = in ? a[h][i] : u32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int j = 0; j < TN; ++j) b[j] = st[(n0 + j * 16 + r16) * 8 + c];
-                if (l * 128 + 128 > bytes) {                             // the row ends in this line
-                    const bool in = l * 128 + (h * 4 + kq) * 16 < bytes;
-#pragma unroll
-                    for (int i = 0; i < TM; ++i) a[i] = in ? a[i] : u32x4{0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) b[j] = in ? b[j] : u32x4{0, 0, 0, 0};
-                }
-#pragma unroll
-                for (int i = 0; i < TM; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j) acc[i][j] = L::mac(a[i], b[j], acc[i][j]);
+                for (int j = 0; j < TN; ++j) b[h][j] = in ? b[h][j] : u32x4{0, 0, 0, 0};
             }
-            free = now;
-            now = now + 1 == S ? 0 : now + 1;
         }
+        multiply(0);
+        multiply(1);
         asm volatile("s_waitcnt vmcnt(0)" : : : "memory");               // the last loads are through before the workgroup ends
     }
     // (a first part without lines: its sum is the zero that acc starts from)
-    float *out = p.logits + (size_t)quarter * p.T * p.E;
+    float *out = p.logits + (size_t)slice * p.T * p.E;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int e = e0 + n0 - TILE_TOKENS + j * 16 + r16;
@@ -203,7 +224,7 @@ __global__ void __launch_bounds__(TILE_WAVES * 64, 2) router_tile_kernel(RouterP
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int t = t0 + m0 + i * 16 + 4 * kq + v;
-                if (t < p.T) out[(size_t)t * p.E + e] = first[i][j][v] + acc[i][j][v];
+                if (t < p.T) out[(size_t)t * p.E + e] = TAKE == 2 ? first[i][j][v] + acc[i][j][v] : acc[i][j][v];
             }
     }
 }
@@ -239,6 +260,13 @@ __device__ __forceinline__ float row_sum(float v) {
     return read_lane(v, 63);
 }
 
+// e^x: 2^(x log2 e) with the rest of the product, which the instruction's argument has no room for
+__device__ __forceinline__ float exponential(float x) {
+    const float hi = x * 0x1.715476p+0f, lo = fmaf(x, 0x1.715476p+0f, -hi) + x * 0x1.4ae0c0p-26f;    // log2 e in two parts
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return fabsf(hi) < 120.0f ? fmaf(e, lo * 0x1.62e430p-1f, e) : e;                                 // 2^lo = 1 + lo log 2
+}
+
 struct Two {                               // the largest and second largest of a set
     float first, second;
     __device__ __forceinline__ void join(float f, float g) {
@@ -246,6 +274,18 @@ struct Two {                               // the largest and second largest of 
         first = fmaxf(first, f);
     }
 };
+
+// How many groups come before the one that starts at the lane `mine`, `lanes` lanes a group that all hold its two largest
+__device__ __forceinline__ int better_groups(const RouterParams &p, const Two &two, int lanes, int mine) {
+    float score = p.group_top == 2 ? two.first + two.second : two.first;
+    if (!(score == score)) score = -__builtin_inff();
+    int better = 0;
+    for (int g = 0, l = 0; g < p.n_groups; ++g, l += lanes) {
+        const float other = read_lane(score, l);
+        better += (other > score || (other == score && l < mine)) ? 1 : 0;
+    }
+    return better;
+}
 
 // The lane's value v of EC, from a row of n values at a 4-byte address; whole: n is a multiple of EC and the row is at a multiple of
 // EC values
@@ -263,7 +303,7 @@ __device__ __forceinline__ void load_lane(const float *row, int lane, int n, boo
 
 template <int EC, int N>
 __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams p) {
-    __shared__ float choice[SELECT_WAVES][EC * 64];
+    __shared__ float choice[SELECT_WAVES][EC * 64], score[SELECT_WAVES][EC * 64];
     const int lane = lane_id(), wave = threadIdx.x >> 6, t = blockIdx.x * SELECT_WAVES + wave;
     if (t >= p.T) return;
     const float NEVER = -__builtin_inff();
@@ -286,7 +326,7 @@ __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams 
     }
     if (p.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < EC; ++i) s[i] = 1.0f / (1.0f + expf(-s[i]));
+        for (int i = 0; i < EC; ++i) s[i] = __builtin_amdgcn_rcpf(1.0f + exponential(-s[i]));
     } else {
         uint32_t key = 0;                  // (a NaN among the logits makes every score one, by the sum)
 #pragma unroll
@@ -295,28 +335,27 @@ __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams 
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < EC; ++i) {
-            s[i] = lane * EC + i < E ? expf(s[i] - most) : 0.0f;
+            s[i] = lane * EC + i < E ? exponential(s[i] - most) : 0.0f;
             sum += s[i];
         }
-        sum = row_sum(sum);
+        const float inv = 1.0f / row_sum(sum);
 #pragma unroll
-        for (int i = 0; i < EC; ++i) s[i] = s[i] / sum;
+        for (int i = 0; i < EC; ++i) s[i] *= inv;
     }
-    // choices as ordered integers (0: never chosen), sorted by the lane
-    uint32_t key[EC];
+    // choices as ordered integers (0: never chosen), sorted by the lane; order: which of its experts, a byte each
+    uint32_t key[EC], order = 0;
     int at[EC];
 #pragma unroll
     for (int i = 0; i < EC; ++i) {
-        at[i] = lane * EC + i;
+        at[i] = i;
         c[i] = s[i] + c[i];
-        if (at[i] >= E || !(c[i] == c[i])) c[i] = NEVER;
+        if (lane * EC + i >= E || !(c[i] == c[i])) c[i] = NEVER;
         key[i] = c[i] == NEVER ? 0u : float_to_ordered(c[i]);
+        score[wave][lane * EC + i] = s[i];
     }
     const bool grouped = p.keep_groups < p.n_groups;
-    const int per = E / p.n_groups;
-    const int lanes = EC == 1 ? per : per % EC == 0 ? per / EC : 0;
-    const bool in_lanes = grouped && lanes > 0 && (lanes & (lanes - 1)) == 0;      // a group is a power of two of lanes
-    if (grouped && !in_lanes) {
+    const int per = p.per_group, lanes = p.lanes_per_group;                         // lanes: 0, or a power of two that holds a group
+    if (grouped && lanes == 0) {
 #pragma unroll
         for (int i = 0; i < EC; ++i) choice[wave][lane * EC + i] = c[i];
     }
@@ -326,29 +365,20 @@ __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams 
         for (int i = 0; i < EC - 1 - pass; ++i) {
             const bool swap = key[i + 1] > key[i];
             const uint32_t k0 = key[i];
-            const float s0 = s[i];
             const int a0 = at[i];
             key[i] = swap ? key[i + 1] : k0;
-            s[i] = swap ? s[i + 1] : s0;
             at[i] = swap ? at[i + 1] : a0;
             key[i + 1] = swap ? k0 : key[i + 1];
-            s[i + 1] = swap ? s0 : s[i + 1];
             at[i + 1] = swap ? a0 : at[i + 1];
         }
-    if (in_lanes) {
+    if (grouped && lanes > 0) {
         Two two{key[0] ? ordered_to_float(key[0]) : NEVER, EC > 1 && key[EC > 1] ? ordered_to_float(key[EC > 1]) : NEVER};
         if (lanes > 1) two.join(dpp<0xB1>(0.f, two.first), dpp<0xB1>(0.f, two.second));
         if (lanes > 2) two.join(dpp<0x4E>(0.f, two.first), dpp<0x4E>(0.f, two.second));
         if (lanes > 4) two.join(dpp<0x141>(0.f, two.first), dpp<0x141>(0.f, two.second));
         if (lanes > 8) two.join(dpp<0x140>(0.f, two.first), dpp<0x140>(0.f, two.second));
         if (lanes > 16) two.join(__shfl_xor(two.first, 16, WAVE), __shfl_xor(two.second, 16, WAVE));
-        float score = p.group_top == 2 ? two.first + two.second : two.first;
-        if (!(score == score)) score = NEVER;
-        int better = 0;
-        for (int g = 0, l = 0; g < p.n_groups; ++g, l += lanes) {
-            const float other = read_lane(score, l);
-            better += (other > score || (other == score && l < (lane & -lanes))) ? 1 : 0;
-        }
+        const int better = better_groups(p, two, lanes, lane & -lanes);
 #pragma unroll
         for (int i = 0; i < EC; ++i) key[i] = better < p.keep_groups ? key[i] : 0u;
     } else if (grouped) {
@@ -361,54 +391,45 @@ __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams 
         if (group < p.n_groups)
             for (int j = sub; j < per; j += 1 << shift) two.join(choice[wave][group * per + j], NEVER);
         for (int m = 1; m < 1 << shift; m <<= 1) two.join(__shfl_xor(two.first, m, WAVE), __shfl_xor(two.second, m, WAVE));
-        float score = p.group_top == 2 ? two.first + two.second : two.first;
-        if (!(score == score)) score = NEVER;
-        int better = 0;
-        for (int g = 0; g < p.n_groups; ++g) {
-            const float other = read_lane(score, g << shift);
-            better += (other > score || (other == score && g < group)) ? 1 : 0;
-        }
+        const int better = better_groups(p, two, 1 << shift, group << shift);
         const unsigned long long kept = __ballot(better < p.keep_groups && group < p.n_groups);
 #pragma unroll
         for (int i = 0; i < EC; ++i)
-            if (key[i] && !(kept >> ((at[i] / per) << shift) & 1)) key[i] = 0;
+            if (key[i] && !(kept >> (((lane * EC + at[i]) / per) << shift) & 1)) key[i] = 0;
         // those that are out move behind the others, which stay in order
 #pragma unroll
         for (int pass = 0; pass < EC - 1; ++pass)
 #pragma unroll
             for (int i = 0; i < EC - 1 - pass; ++i) {
                 const bool swap = key[i] == 0;
-                const float s0 = s[i];
                 const int a0 = at[i];
                 key[i] = swap ? key[i + 1] : key[i];
-                s[i] = swap ? s[i + 1] : s[i];
                 at[i] = swap ? at[i + 1] : at[i];
                 key[i + 1] = swap ? 0u : key[i + 1];
-                s[i + 1] = swap ? s0 : s[i + 1];
                 at[i + 1] = swap ? a0 : at[i + 1];
             }
     }
-    int32_t id = -1;
-    float w = 0.0f, total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < EC; ++i) order |= (uint32_t)at[i] << 8 * i;
+    int id = -1;                           // of slot `lane`
     for (int k = 0; k < p.K; ++k) {
         const uint32_t most = wave_max_u32(key[0]);
         if (most == 0) break;
         const int from = __builtin_ctzll(__ballot(key[0] == most));
-        const float sw = read_lane(s[0], from);
-        const int e = __builtin_amdgcn_readlane(at[0], from);
-        total += sw;
+        const int e = EC == 1 ? from : from * EC + (__builtin_amdgcn_readlane((int)order, from) & 0xff);
         id = lane == k ? e : id;
-        w = lane == k ? sw : w;
         if (lane == from) {
 #pragma unroll
-            for (int i = 0; i < EC; ++i) {
-                key[i] = i + 1 < EC ? key[(i + 1) % EC] : 0u;
-                s[i] = s[(i + 1) % EC];
-                at[i] = at[(i + 1) % EC];
-            }
+            for (int i = 0; i < EC; ++i) key[i] = i + 1 < EC ? key[(i + 1) % EC] : 0u;
+            order >>= 8;
         }
     }
-    if (p.renorm) w = w / (total < 0x1p-126f ? 0x1p-126f : total);
+    wave_lds_fence();
+    float w = id >= 0 ? score[wave][id] : 0.0f;
+    if (p.renorm) {
+        const float total = row_sum(w);
+        w = w / (total < 0x1p-126f ? 0x1p-126f : total);
+    }
     if (lane < p.K) {
         p.ids[(size_t)t * p.K + lane] = id;
         p.weights[(size_t)t * p.K + lane] = w * p.scale;
@@ -416,56 +437,83 @@ __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams 
 }
 
 template <int N>
-void launch_select(const RouterParams &p, hipStream_t st) {
+void launch_select(RouterParams p, hipStream_t st) {
+    p.per_group = p.E / p.n_groups;
+    const int ec = p.E <= 64 ? 1 : p.E <= 128 ? 2 : 4, lanes = p.per_group % ec == 0 ? p.per_group / ec : 0;
+    p.lanes_per_group = (lanes & (lanes - 1)) == 0 ? lanes : 0;
     const dim3 grid((p.T + SELECT_WAVES - 1) / SELECT_WAVES), block(SELECT_WAVES * 64);
     if (p.E <= 64) hipLaunchKernelGGL((select_kernel<1, N>), grid, block, 0, st, p);
     else if (p.E <= 128) hipLaunchKernelGGL((select_kernel<2, N>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((select_kernel<4, N>), grid, block, 0, st, p);
 }
 
-template <typename L, int EB>
+template <typename L, int EB, int TAKE>
 void launch_tile(const RouterParams &p, hipStream_t st) {
-    const int pairs = (p.T + 2 * TILE_TOKENS - 1) / (2 * TILE_TOKENS);     // of token tiles: one for each half of the dies
-    hipLaunchKernelGGL((router_tile_kernel<L, EB>), dim3((p.E + EB - 1) / EB * pairs * 8), dim3(TILE_WAVES * 64), RouterTile<EB>::LDS, st, p);
-}
-
-template <typename L>
-void launch_tiles(const RouterParams &p, hipStream_t st) {
-    if (p.E <= 32) launch_tile<L, 32>(p, st);
-    else if (p.E <= 64) launch_tile<L, 64>(p, st);
-    else if (p.E <= 128) launch_tile<L, 128>(p, st);
-    else launch_tile<L, 256>(p, st);
+    const int tiles = (p.T + TILE_TOKENS * TAKE - 1) / (TILE_TOKENS * TAKE);      // of each die
+    hipLaunchKernelGGL((router_tile_kernel<L, EB, TAKE>), dim3((p.E + EB - 1) / EB * tiles * 8), dim3(TILE_WAVES * 64), RouterTile<EB>::LDS, st, p);
 }
 
 constexpr int CHUNK = 16384;             // tokens whose logits lie in the scratch at once
-constexpr int TILED_FROM = 1024;
+
+// From how many logits on the product is tiled: small | tiled product, us of the whole call.  bf16: 4096 -> 256 experts at 32 / 64 / 128 / 256
+// tokens 7.3 8.2 10.2 14.2 | 8.7 8.8 9.0 9.7, 2048 -> 128 at 64 / 128 / 256 6.6 7.7 9.9 | 7.1 7.5 8.0, 2048 -> 64 at 128 / 256 / 512
+// 6.1 7.1 9.1 | 6.7 7.0 7.4, 4096 -> 8 at 1024 / 2048 6.8 8.8 | 7.6 7.8.  fp32: 2048 -> 256 at 128 / 256 10.7 14.8 | 12.1 12.8,
+// 2048 -> 128 at 256 / 512 10.5 14.6 | 11.9 12.8, 1440 -> 60 at 512 / 1024 9.3 13.7 | 9.7 10.3.
+bool wants_tiles(int T, int E, bool f32) { return (long long)T * E >= (f32 ? 40960 : 16384); }
+
+// A tiled product's workgroup takes one of the eight parts of the reduction, or of large batches two: half of the parts to write and to
+// read, but half of the workgroups.  One | two, us: 4096 -> 256 at 1024 / 2048 / 4096 tokens 14.2 20.5 26.7 | 23.3 25.5 31.0,
+// 4096 -> 8 at 4096 9.4 | 13.6; fewer lines: 2048 -> 128 at 2048 / 4096 12.5 19.1 | 13.3 14.9, 2048 -> 64 9.2 12.6 | 9.4 10.7;
+// fp32: 2048 -> 128 at 4096 32.1 | 46.8, 1440 -> 60 16.9 | 20.8.
+constexpr int EIGHTHS = 4096;
+bool by_eighths(int T, int lines, bool f32) { return T <= (f32 || lines >= 64 ? EIGHTHS : EIGHTHS / 2); }
+
+// All experts in one workgroup, or fewer where that leaves units idle
+template <typename L>
+void launch_tiles(const RouterParams &p, bool eighths, hipStream_t st) {
+    const int tiles = (p.T + TILE_TOKENS - 1) / TILE_TOKENS;
+    if (!eighths) {
+        if (p.E <= 32) launch_tile<L, 32, 2>(p, st);
+        else if (p.E <= 64) launch_tile<L, 64, 2>(p, st);
+        else if (p.E <= 128) launch_tile<L, 128, 2>(p, st);
+        else launch_tile<L, 256, 2>(p, st);
+        return;
+    }
+    auto fits = [&](int eb) { return p.E <= eb || tiles * ((p.E + eb - 1) / eb) * 8 <= 256; };
+    if (fits(32)) launch_tile<L, 32, 1>(p, st);
+    else if (fits(64)) launch_tile<L, 64, 1>(p, st);
+    else if (fits(128)) launch_tile<L, 128, 1>(p, st);
+    else launch_tile<L, 256, 1>(p, st);
+}
 
 }  // namespace
 
 // A larger batch needs no less: eight parts of each logit of a small batch, four of a large one
 size_t router_scratch_bytes(int T, int E) {
-    const size_t few = (size_t)(T < TILED_FROM - 1 ? T : TILED_FROM - 1) * PARTS, many = (size_t)(T < CHUNK ? T : CHUNK) * (PARTS / 2);
+    const size_t few = (size_t)(T < EIGHTHS ? T : EIGHTHS) * PARTS, many = (size_t)(T < CHUNK ? T : CHUNK) * (PARTS / 2);
     return (few > many ? few : many) * E * 4;
 }
 
 int launch_route_scored(const RouterParams &all, bool f32, hipStream_t st) {
     const size_t row = (size_t)all.d * (f32 ? 4 : 2);
     const bool whole = row % 16 == 0 && aligned16(all.x) && aligned16(all.w);
-    // (rows of other lengths and addresses: the product for few tokens, as many at a time as the scratch has room for)
-    const int chunk = whole ? CHUNK : (int)(router_scratch_bytes(all.T, all.E) / ((size_t)PARTS * all.E * 4));
+    const bool tiled = whole && wants_tiles(all.T, all.E, f32), eighths = !tiled || by_eighths(all.T, (int)((row + 127) / 128), f32);
+    // as many tokens at a time as the scratch has room for
+    const int chunk = (int)(router_scratch_bytes(all.T, all.E) / ((size_t)(eighths ? PARTS : PARTS / 2) * all.E * 4));
     for (int t0 = 0; t0 < all.T; t0 += chunk) {
         RouterParams p = all;
         p.T = all.T - t0 < chunk ? all.T - t0 : chunk;
         p.x = static_cast<const char *>(all.x) + t0 * row;
         p.ids = all.ids + (size_t)t0 * p.K;
         p.weights = all.weights + (size_t)t0 * p.K;
-        const dim3 grid((p.E + 15) / 16, (p.T + 15) / 16, PARTS), block(64);
-        if (whole && all.T >= TILED_FROM) {
-            if (f32) launch_tiles<F32Line>(p, st);
-            else launch_tiles<Bf16Line>(p, st);
-            launch_select<PARTS / 2>(p, st);
+        if (tiled) {
+            if (f32) launch_tiles<F32Line>(p, eighths, st);
+            else launch_tiles<Bf16Line>(p, eighths, st);
+            if (eighths) launch_select<PARTS>(p, st);
+            else launch_select<PARTS / 2>(p, st);
             continue;
         }
+        const dim3 grid((p.E + 15) / 16, (p.T + 15) / 16, PARTS), block(64);
         if (!f32) hipLaunchKernelGGL((router_small_kernel<Bf16Line, true>), grid, block, 0, st, p);
         else if (whole) hipLaunchKernelGGL((router_small_kernel<F32Line, true>), grid, block, 0, st, p);
         else hipLaunchKernelGGL((router_small_kernel<F32Line, false>), grid, block, 0, st, p);

@@ -64,10 +64,10 @@ __device__ __forceinline__ int rank_of(const AdapterParams &p, int a) {
 // A row's place among its adapter's rows: those of its wave before it by ballots, and those of earlier waves from counts.
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(ADAPTER_CHUNK) adapter_group_kernel(AdapterParams p) {
-    constexpr int WAVES = ADAPTER_CHUNK / 64;
-    __shared__ uint16_t count[WAVES][BM_MAX_ADAPTERS + 8];
+    constexpr int MOST = ADAPTER_CHUNK / 64;
+    __shared__ uint16_t count[MOST][BM_MAX_ADAPTERS + 8];
     __shared__ int rows_before[BM_MAX_ADAPTERS + 8];
-    __shared__ int wave_rows[WAVES], wave_tiles[WAVES];
+    __shared__ int wave_rows[MOST], wave_tiles[MOST];
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, waves = blockDim.x >> 6, chunk = blockIdx.x;
     const int row = chunk * ADAPTER_CHUNK + tid, keys = p.n + 1;
     for (int k = tid; k < waves * (BM_MAX_ADAPTERS + 8); k += blockDim.x) (&count[0][0])[k] = 0;
@@ -125,92 +125,217 @@ __global__ void __launch_bounds__(ADAPTER_CHUNK) adapter_group_kernel(AdapterPar
 }
 
 // ---------------------------------------------------------------------------
-// u = A x of a tile: the four waves take every fourth line of the workgroup's part of the reduction, their sums are added as
-// (w0 + w2) + (w1 + w3).  Matrix rows are A's, columns the tile's rows: a lane ends with four neighbouring values of u.
-// TS: blocks of 16 rows; NR: blocks of 16 ranks.
+// A workgroup's tile: its adapter and its rows, in LDS.  Up to 64 rows need no grouping: every wave finds the tile by ballots, which takes
+// less than the launch and the round trip to memory of a kernel for it.
 // ---------------------------------------------------------------------------
 constexpr int WAVES = 4;
-constexpr int WANTED = 512, MAX_SPLITS = 16;      // workgroups of the launch, parts of the reduction at most
 
-template <typename L, bool WHOLE, int TS, int NR>
-__device__ __forceinline__ void shrink_tile(const AdapterParams &p, const AdapterTile &tile, int chunk, int split, f32x4 (*sums)[64]) {
+struct TileView {
+    int adapter, count;           // adapter n: rows without one
+    size_t place;                 // FEW: a row's place in u is its number, else place + its number in the tile
+};
+
+template <bool FEW>
+__device__ __forceinline__ bool find_tile(const AdapterParams &p, int *rows, TileView &view) {
+    const int tid = threadIdx.x, lane = lane_id();
+    if constexpr (FEW) {
+        int key = -1;
+        if (lane < p.rows) {
+            key = ldg_i32(p.adapter + lane);
+            if ((unsigned)key >= (unsigned)p.n) key = p.in_place ? -1 : p.n;
+        }
+        unsigned long long left = __ballot(key >= 0), mine = 0;
+        for (int i = 0; i <= (int)blockIdx.x; ++i) {
+            left &= ~mine;
+            if (left == 0) return false;
+            view.adapter = __builtin_amdgcn_readlane(key, __builtin_ctzll(left));
+            mine = __ballot(key == view.adapter);
+        }
+        view.count = __popcll(mine);
+        view.place = 0;
+        if (tid < 64 && key == view.adapter) rows[__popcll(mine & ((1ull << lane) - 1))] = lane;
+    } else {
+        const int chunk = blockIdx.z;
+        if ((int)blockIdx.x >= ldg_i32(p.n_tiles + chunk)) return false;
+        const AdapterTile t = p.tiles[(size_t)chunk * p.max_tiles + blockIdx.x];
+        view.adapter = t.adapter;
+        view.count = t.count;
+        view.place = (size_t)chunk * ADAPTER_CHUNK + t.start;
+        if (tid < t.count) rows[tid] = ldg_i32(p.order + view.place + tid);
+    }
+    return true;
+}
+template <bool FEW>
+__device__ __forceinline__ size_t place_in_u(const TileView &view, const int *rows, int i) { return FEW ? (size_t)rows[i] : view.place + i; }
+
+// ---------------------------------------------------------------------------
+// u = A x of a tile and a part of the reduction.  Matrix rows are A's, columns the tile's rows: a lane ends with four neighbouring values
+// of u.  NR: blocks of 16 ranks.
+// Up to 16 rows: the four waves take every fourth line each, straight from memory, and add their sums as (w0 + w2) + (w1 + w3).
+// More: whole lines of x and A go straight into a ring of LDS stages (row r's 16-byte piece c at slot c ^ (r & 7)), one wait and one
+// barrier a line; the waves share the tile's 64 rows and the ranks.  Direct loads for 64 rows and 128 ranks as well left a wave a
+// SIMD for their registers: 2000 rows of 4096 -> 128 in 28.8 us.
+// ---------------------------------------------------------------------------
+#define BM_LDS __attribute__((address_space(3)))
+
+template <typename L, bool WHOLE, bool FEW, int NR>
+__device__ __forceinline__ void shrink_few(const AdapterParams &p, const TileView &tile, const int *rows, int split, f32x4 (*sums)[64]) {
     const int lane = lane_id(), wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
     const int lines = (p.Kd + L::VALUES - 1) / L::VALUES;
     const int begin = (int)((long long)split * lines / p.splits), end = (int)((long long)(split + 1) * lines / p.splits);
     const int blocks = (rank_of(p, tile.adapter) + 15) >> 4;                  // of ranks that count
-    const char *xr[TS], *ar[NR];
-#pragma unroll
-    for (int i = 0; i < TS; ++i) {
-        const int row = p.order[(size_t)chunk * ADAPTER_CHUNK + tile.start + min(i * 16 + r16, tile.count - 1)];
-        xr[i] = static_cast<const char *>(p.x) + (size_t)row * p.x_stride * L::SIZE;
-    }
+    const char *xr = static_cast<const char *>(p.x) + (size_t)rows[min(r16, tile.count - 1)] * p.x_stride * L::SIZE, *ar[NR];
 #pragma unroll
     for (int j = 0; j < NR; ++j)
         ar[j] = static_cast<const char *>(p.a) + ((size_t)tile.adapter * p.rank + min(j * 16 + r16, p.rank - 1)) * p.Kd * L::SIZE;
-    f32x4 acc[NR][TS];
+    f32x4 acc[NR];
 #pragma unroll
-    for (int j = 0; j < NR; ++j)
-#pragma unroll
-        for (int i = 0; i < TS; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NR; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int l = begin + wave; l < end; l += WAVES) {
-        u32x4 xv[TS][2], av[NR][2];
+        u32x4 xv[2], av[NR][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = l * L::VALUES + (h * 4 + kq) * (16 / L::SIZE);
-#pragma unroll
-            for (int i = 0; i < TS; ++i) xv[i][h] = piece<L, WHOLE>(xr[i], at, p.Kd, p.Kd);
+            xv[h] = piece<L, WHOLE>(xr, at, p.Kd, p.Kd);
 #pragma unroll
             for (int j = 0; j < NR; ++j)
                 if (j < blocks) av[j][h] = piece<L, WHOLE>(ar[j], at, p.Kd, p.Kd);
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int j = 0; j < NR; ++j) {
+            if (j >= blocks) break;
 #pragma unroll
-            for (int j = 0; j < NR; ++j) {
-                if (j >= blocks) break;
-#pragma unroll
-                for (int i = 0; i < TS; ++i) acc[j][i] = L::mac(av[j][h], xv[i][h], acc[j][i]);
-            }
+            for (int h = 0; h < 2; ++h) acc[j] = L::mac(av[j][h], xv[h], acc[j]);
+        }
     }
     if (wave >= 2)
 #pragma unroll
-        for (int j = 0; j < NR; ++j)
-#pragma unroll
-            for (int i = 0; i < TS; ++i) sums[((wave - 2) * NR + j) * TS + i][lane] = acc[j][i];
+        for (int j = 0; j < NR; ++j) sums[(wave - 2) * NR + j][lane] = acc[j];
     __syncthreads();
     if (wave < 2)
 #pragma unroll
-        for (int j = 0; j < NR; ++j)
-#pragma unroll
-            for (int i = 0; i < TS; ++i) {
-                f32x4 &other = sums[(wave * NR + j) * TS + i][lane];
-                acc[j][i] += other;
-                if (wave == 1) other = acc[j][i];
-            }
+        for (int j = 0; j < NR; ++j) {
+            f32x4 &other = sums[wave * NR + j][lane];
+            acc[j] += other;
+            if (wave == 1) other = acc[j];
+        }
     __syncthreads();
-    if (wave != 0) return;
-    float *u = p.u + (split * (size_t)p.u_rows + (size_t)chunk * ADAPTER_CHUNK) * p.width;
+    if (wave != 0 || r16 >= tile.count) return;
+    float *u = p.u + (split * (size_t)p.u_rows + place_in_u<FEW>(tile, rows, r16)) * p.width;
 #pragma unroll
     for (int j = 0; j < NR; ++j) {
         if (j >= blocks) break;
-#pragma unroll
-        for (int i = 0; i < TS; ++i) {
-            const f32x4 sum = acc[j][i] + sums[(NR + j) * TS + i][lane];
-            if (i * 16 + r16 < tile.count)
-                *(BM_GLOBAL f32x4 *)(u + (size_t)(tile.start + i * 16 + r16) * p.width + j * 16 + kq * 4) = sum;
-        }
+        *(BM_GLOBAL f32x4 *)(u + j * 16 + kq * 4) = acc[j] + sums[NR + j][lane];
     }
 }
 
-template <typename L, bool WHOLE, int NR>
+template <int NR>
+struct Ring {
+    static constexpr int RB = NR * 16, ROWS = ADAPTER_TILE;
+    static constexpr int WN = NR >= 4 ? 2 : 1, WM = WAVES / WN;                          // waves along ranks and rows
+    static constexpr int TM = ROWS / WM / 16, TN = NR / WN;                              // 16 x 16 blocks of a wave
+    static constexpr int BLOCKS = (ROWS + RB) / 8, LOADS = (BLOCKS + WAVES - 1) / WAVES; // of 8 rows; a wave and stage
+    static constexpr int STAGES = NR == 8 ? 3 : 4, STAGE = BLOCKS * 64;                  // 16-byte pieces of a stage: two to four workgroups a unit
+};
+
+template <typename L, bool FEW, int NR>
+__device__ __forceinline__ void shrink_ring(const AdapterParams &p, const TileView &tile, const int *rows, int split, u32x4 *smem) {
+    using R = Ring<NR>;
+    constexpr int S = R::STAGES, TM = R::TM, TN = R::TN;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, kq = lane >> 4;
+    const int bytes = p.Kd * L::SIZE, lines = (bytes + 127) >> 7, rank = rank_of(p, tile.adapter);
+    const int begin = (int)((long long)split * lines / p.splits), end = (int)((long long)(split + 1) * lines / p.splits);
+    if (begin >= end || rank == 0) return;                                   // (splits <= lines: no part is empty)
+    const char *from[R::LOADS];
+    int to[R::LOADS];
+#pragma unroll
+    for (int j = 0; j < R::LOADS; ++j) {
+        int block = wave + WAVES * j;
+        if (block >= R::BLOCKS) block = wave % R::BLOCKS;                    // (a repeated load of what is there)
+        const int row = block * 8 + (lane >> 3);
+        from[j] = row < R::ROWS ? static_cast<const char *>(p.x) + (size_t)rows[min(row, tile.count - 1)] * p.x_stride * L::SIZE
+                                : static_cast<const char *>(p.a) + ((size_t)tile.adapter * p.rank + min(row - R::ROWS, rank - 1)) * bytes;
+        to[j] = block * 64;
+    }
+    const int piece_at = ((lane & 7) ^ (lane >> 3)) * 16;
+    auto load = [&](int l, int slot) {
+        const int at = min(l, end - 1) * 128 + piece_at, within = at < bytes ? at : 0;   // (behind a row's end: cleared when read)
+#pragma unroll
+        for (int j = 0; j < R::LOADS; ++j)
+            __builtin_amdgcn_global_load_lds((const BM_GLOBAL void *)(from[j] + within), (BM_LDS void *)(smem + slot * R::STAGE + to[j]), 16, 0, 0);
+    };
+    const int m0 = wave % R::WM * (TM * 16), n0 = wave / R::WM * (TN * 16);
+    const bool idle = m0 >= tile.count || n0 >= rank;                        // (the wave's part of the tile holds nothing)
+    f32x4 acc[TN][TM];
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) load(begin + i, i);
+    int now = 0, free = S - 1;
+    for (int l = begin; l < end; ++l) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
+        load(l + S - 1, free);
+        const u32x4 *st = smem + now * R::STAGE;
+        if (!idle)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                u32x4 x[TM], a[TN];
+                const int c = (h * 4 + kq) ^ (r16 & 7);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) x[i] = st[(m0 + i * 16 + r16) * 8 + c];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) a[j] = st[(R::ROWS + n0 + j * 16 + r16) * 8 + c];
+                if (l * 128 + 128 > bytes) {                                 // the row ends in this line
+                    const bool in = l * 128 + (h * 4 + kq) * 16 < bytes;
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) x[i] = in ? x[i] : u32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) a[j] = in ? a[j] : u32x4{0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i) acc[j][i] = L::mac(a[j], x[i], acc[j][i]);
+            }
+        free = now;
+        now = now + 1 == S ? 0 : now + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" : : : "memory");                       // the last loads are through before the workgroup ends
+    if (idle) return;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int row = m0 + i * 16 + r16;
+        if (row >= tile.count) continue;
+        float *u = p.u + (split * (size_t)p.u_rows + place_in_u<FEW>(tile, rows, row)) * p.width + n0 + kq * 4;
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+            if (n0 + j * 16 < rank) *(BM_GLOBAL f32x4 *)(u + j * 16) = acc[j][i];
+    }
+}
+
+template <typename L, bool WHOLE, bool FEW, int NR>
 __global__ void __launch_bounds__(WAVES * 64) adapter_shrink_kernel(AdapterParams p) {
-    __shared__ f32x4 sums[2 * NR * (ADAPTER_TILE / 16)][64];
-    const int chunk = blockIdx.z;
-    if ((int)blockIdx.x >= ldg_i32(p.n_tiles + chunk)) return;
-    const AdapterTile tile = p.tiles[(size_t)chunk * p.max_tiles + blockIdx.x];
-    if (tile.adapter >= p.n) return;
-    if (tile.count <= 16) shrink_tile<L, WHOLE, 1, NR>(p, tile, chunk, blockIdx.y, sums);
-    else shrink_tile<L, WHOLE, ADAPTER_TILE / 16, NR>(p, tile, chunk, blockIdx.y, sums);
+    using R = Ring<NR>;
+    __shared__ u32x4 smem[WHOLE ? R::STAGES * R::STAGE : 2 * NR * 64];
+    static_assert(R::STAGES * R::STAGE >= 2 * NR * 64, "holds the waves' sums of up to 16 rows");
+    __shared__ int rows[ADAPTER_TILE];
+    TileView tile;
+    if (!find_tile<FEW>(p, rows, tile) || tile.adapter >= p.n) return;
+    __syncthreads();
+    f32x4(*sums)[64] = reinterpret_cast<f32x4(*)[64]>(smem);
+    if constexpr (WHOLE) {
+        if (tile.count > 16) shrink_ring<L, FEW, NR>(p, tile, rows, blockIdx.y, smem);
+        else shrink_few<L, true, FEW, NR>(p, tile, rows, blockIdx.y, sums);
+    } else {
+        // other lengths and addresses: 16 rows at a time
+        for (int i = 0; i < tile.count; i += 16) {
+            TileView part{tile.adapter, min(16, tile.count - i), tile.place + i};
+            shrink_few<L, false, FEW, NR>(p, part, rows + i, blockIdx.y, sums);
+            __syncthreads();
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -241,28 +366,42 @@ __device__ __forceinline__ uint32_t take_bf16(float &a, float &b) {
     return v;
 }
 
-template <typename L, bool YF32, int NR>
-__device__ __forceinline__ void stage_u(const AdapterParams &p, const AdapterTile &tile, int chunk, int rank, Expanded<L, YF32, NR> &out) {
+template <typename L, bool YF32, bool FEW, int NR>
+__device__ __forceinline__ void stage_u(const AdapterParams &p, const TileView &tile, const int *rows, int rank, Expanded<L, YF32, NR> &out) {
     using X = Expanded<L, YF32, NR>;
+    constexpr int Q = X::F32 ? 1 : 2;                        // pieces of four ranks: 8 ranks in bf16, 4 in fp32
     const size_t step = (size_t)p.u_rows * p.width;
     const int blocks = (tile.count + 15) >> 4;
-    // a thread makes one lane's piece of a k block: 8 ranks in bf16, 4 in fp32
     for (int at = threadIdx.x; at < X::KB * blocks * 64; at += WAVES * 64) {
         const int lane = at & 63, i = (at >> 6) % blocks, kb = (at >> 6) / blocks;
         const int kq = lane >> 4, row = min(i * 16 + (lane & 15), tile.count - 1);
         const int r0 = X::F32 ? kb * 16 + kq * 4 : NR == 1 ? (kq & 1) * 8 : kb * 32 + kq * 8;
-        const float *u = p.u + ((size_t)chunk * ADAPTER_CHUNK + tile.start + row) * p.width + r0;
+        const float *u = p.u + place_in_u<FEW>(tile, rows, row) * p.width;
+        f32x4 sum[Q];
+        int from[Q];
+#pragma unroll
+        for (int h = 0; h < Q; ++h) {
+            sum[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+            from[h] = r0 + 4 * h < rank ? r0 + 4 * h : 0;    // (blocks of 16 ranks behind the last one are not written)
+        }
+        for (int s0 = 0; s0 < p.splits; s0 += 4) {           // four parts' loads on their way
+            f32x4 v[4][Q];
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int h = 0; h < Q; ++h) v[s][h] = *(const BM_GLOBAL f32x4 *)(u + min(s0 + s, p.splits - 1) * step + from[h]);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if (s0 + s >= p.splits) break;
+#pragma unroll
+                for (int h = 0; h < Q; ++h) sum[h] += v[s][h];
+            }
+        }
         float v[8];
 #pragma unroll
-        for (int h = 0; h < (X::F32 ? 1 : 2); ++h) {
-            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-            if (r0 + 4 * h < rank) {                         // (blocks of 16 ranks behind the last one are not written)
-                sum = *(const BM_GLOBAL f32x4 *)(u + 4 * h);
-                for (int s = 1; s < p.splits; ++s) sum += *(const BM_GLOBAL f32x4 *)(u + s * step + 4 * h);
-            }
+        for (int h = 0; h < Q; ++h)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) v[4 * h + c] = r0 + 4 * h + c < rank ? sum[c] : 0.0f;
-        }
+            for (int c = 0; c < 4; ++c) v[4 * h + c] = r0 + 4 * h + c < rank ? sum[h][c] : 0.0f;
         if constexpr (X::F32) {
             out.v[0][kb][i][lane] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
         } else {
@@ -283,74 +422,80 @@ __device__ __forceinline__ void stage_u(const AdapterParams &p, const AdapterTil
     }
 }
 
-// N values of a row of y from column n on, as fp32
-template <bool YF32, bool WHOLE, int N>
-__device__ __forceinline__ void load_row(const void *row, int n, int end, float (&v)[N]) {
-    if constexpr (WHOLE) {
-        if (n < end) {
-            if constexpr (YF32) {
+// Eight values of a row of base or y from column n on (a multiple of 8), as they lie in memory
+template <bool YF32>
+struct Eight {
+    u32x4 v[YF32 ? 2 : 1];
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const char *row, int n, int end) {
+        constexpr int SIZE = YF32 ? 4 : 2, PER = 16 / SIZE;
 #pragma unroll
-                for (int i = 0; i < N; i += 4) {
-                    const f32x4 q = *(const BM_GLOBAL f32x4 *)(static_cast<const float *>(row) + (n + i < end ? n + i : n));
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) v[i + c] = q[c];
-                }
+        for (int i = 0; i < 8 / PER; ++i) {
+            const int at = n + i * PER;
+            if constexpr (WHOLE) {
+                v[i] = ldg128(row + (size_t)(at < end ? at : 0) * SIZE);
             } else {
-                const u32x4 q = ldg128(static_cast<const uint16_t *>(row) + n);
+                v[i] = u32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = bf16_to_f32((uint16_t)(q[i / 2] >> 16 * (i % 2)));
+                for (int c = 0; c < PER; ++c)
+                    if (at + c < end) {
+                        if constexpr (YF32) v[i][c] = (uint32_t)ldg_i32(row + (size_t)(at + c) * 4);
+                        else v[i][c / 2] |= (uint32_t)*(const BM_GLOBAL uint16_t *)(row + (size_t)(at + c) * 2) << 16 * (c % 2);
+                    }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = 0.0f;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = 0.0f;
-            if (n + i < end) v[i] = YF32 ? ldg_f32(static_cast<const float *>(row) + n + i)
-                                         : bf16_to_f32(*(const BM_GLOBAL uint16_t *)(static_cast<const uint16_t *>(row) + n + i));
         }
     }
-}
-
-template <bool YF32, bool WHOLE, int N>
-__device__ __forceinline__ void store_row(void *row, int n, int end, const float (&v)[N]) {
-    if constexpr (WHOLE) {
+    template <bool WHOLE>
+    __device__ __forceinline__ void store(char *row, int n, int end) const {
+        constexpr int SIZE = YF32 ? 4 : 2, PER = 16 / SIZE;
+#pragma unroll
+        for (int i = 0; i < 8 / PER; ++i) {
+            const int at = n + i * PER;
+            if constexpr (WHOLE) {
+                if (at < end) stg128(row + (size_t)at * SIZE, v[i]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < PER; ++c)
+                    if (at + c < end) {
+                        if constexpr (YF32) *(BM_GLOBAL uint32_t *)(row + (size_t)(at + c) * 4) = v[i][c];
+                        else stg16(row + (size_t)(at + c) * 2, (uint16_t)(v[i][c / 2] >> 16 * (c % 2)));
+                    }
+            }
+        }
+    }
+    // + scale * (a, b)
+    __device__ __forceinline__ void add(float scale, f32x4 a, f32x4 b) {
+        float f[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const uint32_t bits = YF32 ? v[c / 4 % (YF32 ? 2 : 1)][c % 4] : v[0][c / 2 % 4] >> 16 * (c % 2) << 16;
+            const float base = __builtin_bit_cast(float, bits);
+            f[c] = fmaf(scale, c < 4 ? a[c % 4] : b[c % 4], base);
+        }
         if constexpr (YF32) {
 #pragma unroll
-            for (int i = 0; i < N; i += 4)
-                if (n + i < end) *(BM_GLOBAL f32x4 *)(static_cast<float *>(row) + n + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
-        } else if (n < end) {
-            u32x4 q;
+            for (int c = 0; c < 8; ++c) v[c / 4][c % 4] = __builtin_bit_cast(uint32_t, f[c]);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-            stg128(static_cast<uint16_t *>(row) + n, q);
+            for (int c = 0; c < 4; ++c) v[0][c] = pack_bf16x2(f[2 * c], f[2 * c + 1]);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (n + i < end) {
-                if (YF32) *(BM_GLOBAL float *)(static_cast<float *>(row) + n + i) = v[i];
-                else stg16(static_cast<uint16_t *>(row) + n + i, f32_to_bf16(v[i]));
-            }
     }
-}
+};
 
-template <typename L, bool WHOLE, bool YF32, bool YWHOLE, int NR>
+template <typename L, bool WHOLE, bool YF32, bool YWHOLE, bool FEW, int NR>
 __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParams p) {
     using X = Expanded<L, YF32, NR>;
+    constexpr int BLOCKS = ADAPTER_TILE / 16, YSIZE = YF32 ? 4 : 2;
     __shared__ X s;
-    const int chunk = blockIdx.z;
-    if ((int)blockIdx.x >= ldg_i32(p.n_tiles + chunk)) return;
-    const AdapterTile tile = p.tiles[(size_t)chunk * p.max_tiles + blockIdx.x];
+    __shared__ int rows[ADAPTER_TILE];
+    TileView tile;
+    if (!find_tile<FEW>(p, rows, tile)) return;
     const int lane = lane_id(), wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
     const bool none = tile.adapter >= p.n;                   // rows without an adapter: base goes to y
     const int rank = none ? 0 : rank_of(p, tile.adapter);
     const float scale = none || p.scale == nullptr ? 1.0f : ldg_f32(p.scale + tile.adapter);
     const int n0 = blockIdx.y * RANGE + wave * 64, blocks = (tile.count + 15) >> 4;
-    const int ysize = YF32 ? 4 : 2;
-    if (rank > 0) stage_u<L, YF32, NR>(p, tile, chunk, rank, s);
+    // everything that does not wait for u is on its way before it: B's rows, and base's of all of the tile
     u32x4 bv[X::KB][4];
     if (rank > 0 && n0 < p.N) {
 #pragma unroll
@@ -365,14 +510,24 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParam
         }
     }
     __syncthreads();
-    if (n0 >= p.N) return;
-    for (int i = 0; i < blocks; ++i) {
-        const bool live = i * 16 + r16 < tile.count;
-        const int row = p.order[(size_t)chunk * ADAPTER_CHUNK + tile.start + min(i * 16 + r16, tile.count - 1)];
-        const char *from = static_cast<const char *>(p.base) + (size_t)row * p.base_stride * ysize;
-        float v[2][8];
+    Eight<YF32> v[BLOCKS][2];
+    int row[BLOCKS];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) load_row<YF32, YWHOLE>(from, n0 + h * 32 + kq * 8, p.N, v[h]);
+    for (int i = 0; i < BLOCKS; ++i)
+        if (i < blocks) {
+            row[i] = rows[min(i * 16 + r16, tile.count - 1)];
+            const char *from = static_cast<const char *>(p.base) + (size_t)row[i] * p.base_stride * YSIZE;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[i][h].template load<YWHOLE>(from, n0 + h * 32 + kq * 8, p.N);
+        }
+    if (rank > 0) {
+        stage_u<L, YF32, FEW, NR>(p, tile, rows, rank, s);
+        __syncthreads();
+    }
+    if (n0 >= p.N) return;
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+        if (i >= blocks) break;
         if (rank > 0) {
             f32x4 acc[4];
 #pragma unroll
@@ -386,47 +541,43 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParam
                     for (int j = 0; j < 4; ++j) acc[j] = L::mac(bv[kb][j], uv, acc[j]);
                 }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) v[h][c] = fmaf(scale, acc[2 * h + c / 4][c % 4], v[h][c]);
+            for (int h = 0; h < 2; ++h) v[i][h].add(scale, acc[2 * h], acc[2 * h + 1]);
         }
-        char *to = static_cast<char *>(p.y) + (size_t)row * p.y_stride * ysize;
-        if (live)
+        char *to = static_cast<char *>(p.y) + (size_t)row[i] * p.y_stride * YSIZE;
+        if (i * 16 + r16 < tile.count)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) store_row<YF32, YWHOLE>(to, n0 + h * 32 + kq * 8, p.N, v[h]);
+            for (int h = 0; h < 2; ++h) v[i][h].template store<YWHOLE>(to, n0 + h * 32 + kq * 8, p.N);
     }
 }
 
-template <typename L, bool WHOLE, bool YF32, bool YWHOLE, int NR>
-void launch_expand(const AdapterParams &p, hipStream_t st) {
-    hipLaunchKernelGGL((adapter_expand_kernel<L, WHOLE, YF32, YWHOLE, NR>), dim3(p.max_tiles, (p.N + RANGE - 1) / RANGE, p.chunks), dim3(WAVES * 64), 0, st, p);
-}
-
-template <typename L, int NR>
+template <typename L, bool FEW, int NR>
 void launch_rank(const AdapterParams &p, bool y_f32, hipStream_t st) {
     auto whole = [](const void *q, long long values, int size) { return aligned16(q) && values * size % 16 == 0; };
     const bool wx = whole(p.x, p.x_stride, L::SIZE) && whole(p.a, p.Kd, L::SIZE), wb = whole(p.b, p.rank, L::SIZE);
     const int ysize = y_f32 ? 4 : 2;
     const bool wy = whole(p.base, p.base_stride, ysize) && whole(p.y, p.y_stride, ysize) && p.N * ysize % 16 == 0;
-    const dim3 grid(p.max_tiles, p.splits, p.chunks), block(WAVES * 64);
-    if (wx) hipLaunchKernelGGL((adapter_shrink_kernel<L, true, NR>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((adapter_shrink_kernel<L, false, NR>), grid, block, 0, st, p);
+    const dim3 grid(p.max_tiles, p.splits, p.chunks), over(p.max_tiles, (p.N + RANGE - 1) / RANGE, p.chunks), block(WAVES * 64);
+    if (wx) hipLaunchKernelGGL((adapter_shrink_kernel<L, true, FEW, NR>), grid, block, 0, st, p);
+    else hipLaunchKernelGGL((adapter_shrink_kernel<L, false, FEW, NR>), grid, block, 0, st, p);
+    auto expand = [&](auto kernel) { hipLaunchKernelGGL(kernel, over, block, 0, st, p); };
     if (y_f32) {
-        if (wy) wb ? launch_expand<L, true, true, true, NR>(p, st) : launch_expand<L, false, true, true, NR>(p, st);
-        else wb ? launch_expand<L, true, true, false, NR>(p, st) : launch_expand<L, false, true, false, NR>(p, st);
+        if (wy) wb ? expand(adapter_expand_kernel<L, true, true, true, FEW, NR>) : expand(adapter_expand_kernel<L, false, true, true, FEW, NR>);
+        else wb ? expand(adapter_expand_kernel<L, true, true, false, FEW, NR>) : expand(adapter_expand_kernel<L, false, true, false, FEW, NR>);
     } else {
-        if (wy) wb ? launch_expand<L, true, false, true, NR>(p, st) : launch_expand<L, false, false, true, NR>(p, st);
-        else wb ? launch_expand<L, true, false, false, NR>(p, st) : launch_expand<L, false, false, false, NR>(p, st);
+        if (wy) wb ? expand(adapter_expand_kernel<L, true, false, true, FEW, NR>) : expand(adapter_expand_kernel<L, false, false, true, FEW, NR>);
+        else wb ? expand(adapter_expand_kernel<L, true, false, false, FEW, NR>) : expand(adapter_expand_kernel<L, false, false, false, FEW, NR>);
     }
 }
 
-template <typename L>
+template <typename L, bool FEW>
 void launch_typed(const AdapterParams &p, bool y_f32, hipStream_t st) {
-    if (p.width <= 16) launch_rank<L, 1>(p, y_f32, st);
-    else if (p.width <= 32) launch_rank<L, 2>(p, y_f32, st);
-    else if (p.width <= 64) launch_rank<L, 4>(p, y_f32, st);
-    else launch_rank<L, 8>(p, y_f32, st);
+    if (p.width <= 16) launch_rank<L, FEW, 1>(p, y_f32, st);
+    else if (p.width <= 32) launch_rank<L, FEW, 2>(p, y_f32, st);
+    else if (p.width <= 64) launch_rank<L, FEW, 4>(p, y_f32, st);
+    else launch_rank<L, FEW, 8>(p, y_f32, st);
 }
+
+constexpr int WANTED = 512, MAX_SPLITS = 16;      // workgroups of the launch, parts of the reduction at most
 
 }  // namespace
 
@@ -452,10 +603,17 @@ size_t adapter_u_rows(const AdapterParams &p) {
 }
 
 int launch_adapters(const AdapterParams &p, bool f32, bool y_f32, hipStream_t st) {
+    if (p.rows <= ADAPTER_TILE) {
+        AdapterParams few = p;                               // a tile is all rows of an adapter
+        few.max_tiles = p.n + (p.in_place ? 0 : 1) < p.rows ? p.n + (p.in_place ? 0 : 1) : p.rows;
+        if (f32) launch_typed<F32Line, true>(few, y_f32, st);
+        else launch_typed<Bf16Line, true>(few, y_f32, st);
+        return launch_status(__func__);
+    }
     const int threads = p.rows >= ADAPTER_CHUNK ? ADAPTER_CHUNK : (p.rows + 63) / 64 * 64;
     hipLaunchKernelGGL(adapter_group_kernel, dim3(p.chunks), dim3(threads), 0, st, p);
-    if (f32) launch_typed<F32Line>(p, y_f32, st);
-    else launch_typed<Bf16Line>(p, y_f32, st);
+    if (f32) launch_typed<F32Line, false>(p, y_f32, st);
+    else launch_typed<Bf16Line, false>(p, y_f32, st);
     return launch_status(__func__);
 }
 

@@ -26,17 +26,17 @@ struct AdapterParams {
     int rows, Kd, N, n, rank;
     bool in_place;                // base is y: rows without an adapter stay as they are
     int chunks, max_tiles;        // chunks of rows, tiles of a chunk at most
+    int tiles_about;              // of all chunks
     int max_splits;               // whatever the number of rows
     int splits;                   // parts of the reduction over Kd, added in order
     int width;                    // of a row of u: rank rounded up to 16, 32, 64 or 128
     int32_t *order;               // [chunks][ADAPTER_CHUNK] row at each place
-    AdapterTile *tiles;           // [chunks][max_tiles]
-    int32_t *n_tiles;             // [chunks]
+    AdapterTile *tiles;           // [chunks][max_tiles], of no rows behind the last
     float *u;                     // [splits][u_rows][width]: a chunk's rows in its order, from row chunk * ADAPTER_CHUNK on
     long long u_rows;
 };
 
-// The launch for these sizes (rows, Kd, N, n and rank are set): chunks, max_tiles, splits, width and u_rows
+// The launch for these sizes (rows, Kd, N, n and rank are set): chunks, max_tiles, tiles_about, splits, width and u_rows
 void plan_adapters(AdapterParams &p, bool f32);
 size_t adapter_u_rows(const AdapterParams &p);   // room for splits * u_rows, no less for more rows
 int launch_adapters(const AdapterParams &p, bool f32, bool y_f32, hipStream_t st);

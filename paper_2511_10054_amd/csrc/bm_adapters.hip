@@ -62,15 +62,17 @@ __device__ __forceinline__ int rank_of(const AdapterParams &p, int a) {
 // ---------------------------------------------------------------------------
 // The chunk's rows in the order of their adapters, rows of one adapter in their own order, and tiles of up to 64 of them.
 // A row's place among its adapter's rows: those of its wave before it by ballots, and those of earlier waves from counts.
+// Neighbouring tiles - often of one adapter - go to different dies.  (Runs of them on one die read that adapter's matrices once a die,
+// and took 53 us instead of 46 for 8192 rows of 2048 -> 4096, rank 16.)
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(ADAPTER_CHUNK) adapter_group_kernel(AdapterParams p) {
-    constexpr int MOST = ADAPTER_CHUNK / 64;
-    __shared__ uint16_t count[MOST][BM_MAX_ADAPTERS + 8];
-    __shared__ int rows_before[BM_MAX_ADAPTERS + 8];
+    constexpr int MOST = ADAPTER_CHUNK / 64, KEYS = BM_MAX_ADAPTERS + 8;
+    __shared__ uint16_t count[MOST][KEYS];
+    __shared__ int first_row[KEYS], first_tile[KEYS];
     __shared__ int wave_rows[MOST], wave_tiles[MOST];
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, waves = blockDim.x >> 6, chunk = blockIdx.x;
     const int row = chunk * ADAPTER_CHUNK + tid, keys = p.n + 1;
-    for (int k = tid; k < waves * (BM_MAX_ADAPTERS + 8); k += blockDim.x) (&count[0][0])[k] = 0;
+    for (int k = tid; k < waves * KEYS; k += blockDim.x) (&count[0][0])[k] = 0;
     int key = -1;
     if (row < p.rows) {
         key = ldg_i32(p.adapter + row);
@@ -113,15 +115,20 @@ __global__ void __launch_bounds__(ADAPTER_CHUNK) adapter_group_kernel(AdapterPar
             rows_so_far += wr;
             tiles_so_far += wt;
         }
-        const int start = before_rows + r - total, tile0 = before_tiles + t - tiles;
-        if (k < keys) rows_before[k] = start;
-        for (int i = 0; i < tiles; ++i)
-            p.tiles[(size_t)chunk * p.max_tiles + tile0 + i] =
-                AdapterTile{k, start + i * ADAPTER_TILE, min(ADAPTER_TILE, total - i * ADAPTER_TILE), 0};
+        if (k < keys) {
+            first_row[k] = before_rows + r - total;
+            first_tile[k] = before_tiles + t - tiles;
+        }
         __syncthreads();
     }
-    if (key >= 0) p.order[(size_t)chunk * ADAPTER_CHUNK + rows_before[key] + count[wave][key] + rank] = row;
-    if (tid == 0) p.n_tiles[chunk] = tiles_so_far;
+    AdapterTile *const out = p.tiles + (size_t)chunk * p.max_tiles;
+    for (int k = tid; k < keys; k += blockDim.x) {
+        const int start = first_row[k], t0 = first_tile[k];
+        const int total = (k + 1 < keys ? first_row[k + 1] : rows_so_far) - start;
+        for (int i = 0; i * ADAPTER_TILE < total; ++i) out[t0 + i] = AdapterTile{k, start + i * ADAPTER_TILE, min(ADAPTER_TILE, total - i * ADAPTER_TILE), 0};
+    }
+    for (int i = tiles_so_far + tid; i < p.max_tiles; i += blockDim.x) out[i] = AdapterTile{0, 0, 0, 0};
+    if (key >= 0) p.order[(size_t)chunk * ADAPTER_CHUNK + first_row[key] + count[wave][key] + rank] = row;
 }
 
 // ---------------------------------------------------------------------------
@@ -129,6 +136,7 @@ __global__ void __launch_bounds__(ADAPTER_CHUNK) adapter_group_kernel(AdapterPar
 // less than the launch and the round trip to memory of a kernel for it.
 // ---------------------------------------------------------------------------
 constexpr int WAVES = 4;
+constexpr int WANTED = 256, MAX_SPLITS = 8;       // workgroups of the launch, parts of the reduction at most
 
 struct TileView {
     int adapter, count;           // adapter n: rows without one
@@ -156,8 +164,8 @@ __device__ __forceinline__ bool find_tile(const AdapterParams &p, int *rows, Til
         if (tid < 64 && key == view.adapter) rows[__popcll(mine & ((1ull << lane) - 1))] = lane;
     } else {
         const int chunk = blockIdx.z;
-        if ((int)blockIdx.x >= ldg_i32(p.n_tiles + chunk)) return false;
         const AdapterTile t = p.tiles[(size_t)chunk * p.max_tiles + blockIdx.x];
+        if (t.count == 0) return false;
         view.adapter = t.adapter;
         view.count = t.count;
         view.place = (size_t)chunk * ADAPTER_CHUNK + t.start;
@@ -235,7 +243,7 @@ struct Ring {
     static constexpr int WN = NR >= 4 ? 2 : 1, WM = WAVES / WN;                          // waves along ranks and rows
     static constexpr int TM = ROWS / WM / 16, TN = NR / WN;                              // 16 x 16 blocks of a wave
     static constexpr int BLOCKS = (ROWS + RB) / 8, LOADS = (BLOCKS + WAVES - 1) / WAVES; // of 8 rows; a wave and stage
-    static constexpr int STAGES = NR == 8 ? 3 : 4, STAGE = BLOCKS * 64;                  // 16-byte pieces of a stage: two to four workgroups a unit
+    static constexpr int STAGES = NR == 8 ? 3 : 4, STAGE = BLOCKS * 64;   // 16-byte pieces of a stage: two workgroups a unit
 };
 
 template <typename L, bool FEW, int NR>
@@ -339,14 +347,15 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_shrink_kernel(AdapterParam
 }
 
 // ---------------------------------------------------------------------------
-// y = base + scale * B u of a tile and a range of columns.  Matrix rows are B's, columns the tile's rows.  Four matrix blocks cover
-// 64 columns, their rows dealt so that a lane ends with eight neighbouring columns in each half: block j, row 4 q + v is
-// column (j / 2) * 32 + q * 8 + (j % 2) * 4 + v.
+// y = base + scale * B u of a tile and a range of columns.  Matrix rows are B's, columns the tile's rows.  Two matrix blocks cover
+// 32 columns, their rows dealt so that a lane ends with eight neighbouring ones: block j, row 4 q + v is column
+// (j / 2) * 32 + q * 8 + (j % 2) * 4 + v.  A wave takes 64 columns, 32 with ranks beyond 32.
 // bf16: u goes to the matrix unit as the sum of two bf16 values, each the rest of those before it rounded (16 bits of u), of three
 // (all 24) where y is fp32, which would show the difference: 1.6e-6 of an fp32 y with two, rank 128.  Up to 16 ranks the
 // first two lie in one instruction's 32.
 // ---------------------------------------------------------------------------
-constexpr int RANGE = 256;               // columns of a workgroup, 64 a wave
+constexpr int RANGE = 256;               // columns of a workgroup
+constexpr int expand_waves(int nr) { return nr >= 4 ? 8 : 4; }
 
 // The values of u in the form of the matrix operand: [part][k block][row block][lane] 16 bytes
 template <typename L, bool YF32, int NR>
@@ -354,6 +363,7 @@ struct Expanded {
     static constexpr bool F32 = L::SIZE == 4;
     static constexpr int KB = F32 ? NR : (NR + 1) / 2;       // blocks of 16 (fp32) or 32 ranks
     static constexpr int PARTS = F32 ? 1 : NR == 1 ? (YF32 ? 2 : 1) : (YF32 ? 3 : 2);
+    static constexpr int WAVES = expand_waves(NR), H = RANGE / WAVES / 32;   // waves, 32 columns at a time of each
     u32x4 v[PARTS][KB][ADAPTER_TILE / 16][64];
 };
 
@@ -369,10 +379,11 @@ __device__ __forceinline__ uint32_t take_bf16(float &a, float &b) {
 template <typename L, bool YF32, bool FEW, int NR>
 __device__ __forceinline__ void stage_u(const AdapterParams &p, const TileView &tile, const int *rows, int rank, Expanded<L, YF32, NR> &out) {
     using X = Expanded<L, YF32, NR>;
+    constexpr int AHEAD = 4;                                 // (with 8 of them a unit holds fewer waves: 8192 rows 2048 -> 4096 48 -> 52 us)
     constexpr int Q = X::F32 ? 1 : 2;                        // pieces of four ranks: 8 ranks in bf16, 4 in fp32
     const size_t step = (size_t)p.u_rows * p.width;
     const int blocks = (tile.count + 15) >> 4;
-    for (int at = threadIdx.x; at < X::KB * blocks * 64; at += WAVES * 64) {
+    for (int at = threadIdx.x; at < X::KB * blocks * 64; at += X::WAVES * 64) {
         const int lane = at & 63, i = (at >> 6) % blocks, kb = (at >> 6) / blocks;
         const int kq = lane >> 4, row = min(i * 16 + (lane & 15), tile.count - 1);
         const int r0 = X::F32 ? kb * 16 + kq * 4 : NR == 1 ? (kq & 1) * 8 : kb * 32 + kq * 8;
@@ -384,17 +395,17 @@ __device__ __forceinline__ void stage_u(const AdapterParams &p, const TileView &
             sum[h] = f32x4{0.f, 0.f, 0.f, 0.f};
             from[h] = r0 + 4 * h < rank ? r0 + 4 * h : 0;    // (blocks of 16 ranks behind the last one are not written)
         }
-        for (int s0 = 0; s0 < p.splits; s0 += 4) {           // four parts' loads on their way
-            f32x4 v[4][Q];
+        for (int s0 = 0; s0 < p.splits; s0 += AHEAD) {       // so many parts' loads on their way
+            f32x4 w[AHEAD][Q];
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
+            for (int s = 0; s < AHEAD; ++s)
 #pragma unroll
-                for (int h = 0; h < Q; ++h) v[s][h] = *(const BM_GLOBAL f32x4 *)(u + min(s0 + s, p.splits - 1) * step + from[h]);
+                for (int h = 0; h < Q; ++h) w[s][h] = *(const BM_GLOBAL f32x4 *)(u + min(s0 + s, p.splits - 1) * step + from[h]);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
+            for (int s = 0; s < AHEAD; ++s) {
                 if (s0 + s >= p.splits) break;
 #pragma unroll
-                for (int h = 0; h < Q; ++h) sum[h] += v[s][h];
+                for (int h = 0; h < Q; ++h) sum[h] += w[s][h];
             }
         }
         float v[8];
@@ -483,9 +494,9 @@ struct Eight {
 };
 
 template <typename L, bool WHOLE, bool YF32, bool YWHOLE, bool FEW, int NR>
-__global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParams p) {
+__global__ void __launch_bounds__(expand_waves(NR) * 64) adapter_expand_kernel(AdapterParams p) {
     using X = Expanded<L, YF32, NR>;
-    constexpr int BLOCKS = ADAPTER_TILE / 16, YSIZE = YF32 ? 4 : 2;
+    constexpr int BLOCKS = ADAPTER_TILE / 16, YSIZE = YF32 ? 4 : 2, H = X::H;
     __shared__ X s;
     __shared__ int rows[ADAPTER_TILE];
     TileView tile;
@@ -494,12 +505,12 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParam
     const bool none = tile.adapter >= p.n;                   // rows without an adapter: base goes to y
     const int rank = none ? 0 : rank_of(p, tile.adapter);
     const float scale = none || p.scale == nullptr ? 1.0f : ldg_f32(p.scale + tile.adapter);
-    const int n0 = blockIdx.y * RANGE + wave * 64, blocks = (tile.count + 15) >> 4;
+    const int n0 = blockIdx.y * RANGE + wave * (32 * H), blocks = (tile.count + 15) >> 4;
     // everything that does not wait for u is on its way before it: B's rows, and base's of all of the tile
-    u32x4 bv[X::KB][4];
+    u32x4 bv[X::KB][2 * H];
     if (rank > 0 && n0 < p.N) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2 * H; ++j) {
             const int col = n0 + (j / 2) * 32 + (r16 >> 2) * 8 + (j % 2) * 4 + (r16 & 3);
             const char *row = static_cast<const char *>(p.b) + ((size_t)tile.adapter * p.N + min(col, p.N - 1)) * p.rank * L::SIZE;
 #pragma unroll
@@ -510,7 +521,7 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParam
         }
     }
     __syncthreads();
-    Eight<YF32> v[BLOCKS][2];
+    Eight<YF32> v[BLOCKS][H];
     int row[BLOCKS];
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i)
@@ -518,7 +529,7 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParam
             row[i] = rows[min(i * 16 + r16, tile.count - 1)];
             const char *from = static_cast<const char *>(p.base) + (size_t)row[i] * p.base_stride * YSIZE;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[i][h].template load<YWHOLE>(from, n0 + h * 32 + kq * 8, p.N);
+            for (int h = 0; h < H; ++h) v[i][h].template load<YWHOLE>(from, n0 + h * 32 + kq * 8, p.N);
         }
     if (rank > 0) {
         stage_u<L, YF32, FEW, NR>(p, tile, rows, rank, s);
@@ -529,24 +540,24 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_expand_kernel(AdapterParam
     for (int i = 0; i < BLOCKS; ++i) {
         if (i >= blocks) break;
         if (rank > 0) {
-            f32x4 acc[4];
+            f32x4 acc[2 * H];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < 2 * H; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < X::KB; ++kb)
 #pragma unroll
                 for (int part = 0; part < X::PARTS; ++part) {
                     const u32x4 uv = s.v[part][kb][i][lane];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[j] = L::mac(bv[kb][j], uv, acc[j]);
+                    for (int j = 0; j < 2 * H; ++j) acc[j] = L::mac(bv[kb][j], uv, acc[j]);
                 }
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[i][h].add(scale, acc[2 * h], acc[2 * h + 1]);
+            for (int h = 0; h < H; ++h) v[i][h].add(scale, acc[2 * h], acc[2 * h + 1]);
         }
         char *to = static_cast<char *>(p.y) + (size_t)row[i] * p.y_stride * YSIZE;
         if (i * 16 + r16 < tile.count)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) v[i][h].template store<YWHOLE>(to, n0 + h * 32 + kq * 8, p.N);
+            for (int h = 0; h < H; ++h) v[i][h].template store<YWHOLE>(to, n0 + h * 32 + kq * 8, p.N);
     }
 }
 
@@ -559,7 +570,8 @@ void launch_rank(const AdapterParams &p, bool y_f32, hipStream_t st) {
     const dim3 grid(p.max_tiles, p.splits, p.chunks), over(p.max_tiles, (p.N + RANGE - 1) / RANGE, p.chunks), block(WAVES * 64);
     if (wx) hipLaunchKernelGGL((adapter_shrink_kernel<L, true, FEW, NR>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((adapter_shrink_kernel<L, false, FEW, NR>), grid, block, 0, st, p);
-    auto expand = [&](auto kernel) { hipLaunchKernelGGL(kernel, over, block, 0, st, p); };
+    const dim3 wide(expand_waves(NR) * 64);
+    auto expand = [&](auto kernel) { hipLaunchKernelGGL(kernel, over, wide, 0, st, p); };
     if (y_f32) {
         if (wy) wb ? expand(adapter_expand_kernel<L, true, true, true, FEW, NR>) : expand(adapter_expand_kernel<L, false, true, true, FEW, NR>);
         else wb ? expand(adapter_expand_kernel<L, true, true, false, FEW, NR>) : expand(adapter_expand_kernel<L, false, true, false, FEW, NR>);
@@ -577,8 +589,6 @@ void launch_typed(const AdapterParams &p, bool y_f32, hipStream_t st) {
     else launch_rank<L, FEW, 8>(p, y_f32, st);
 }
 
-constexpr int WANTED = 512, MAX_SPLITS = 16;      // workgroups of the launch, parts of the reduction at most
-
 }  // namespace
 
 void plan_adapters(AdapterParams &p, bool f32) {
@@ -587,12 +597,12 @@ void plan_adapters(AdapterParams &p, bool f32) {
     p.max_tiles = rows / ADAPTER_TILE + (keys < rows ? keys : rows);
     p.width = p.rank <= 16 ? 16 : p.rank <= 32 ? 32 : p.rank <= 64 ? 64 : 128;
     p.u_rows = p.chunks > 1 ? (long long)p.chunks * ADAPTER_CHUNK : p.rows;
-    // parts of the reduction: two workgroups a unit, and a line for each of a part's waves
-    const long long tiles = (long long)p.rows / ADAPTER_TILE + (p.n < p.rows ? p.n : p.rows);
-    const long long want = tiles > 0 ? (WANTED + tiles - 1) / tiles : 1;
+    // parts of the reduction: a workgroup a unit, and a line for each of a part's waves
+    p.tiles_about = p.rows / ADAPTER_TILE + (p.n < p.rows ? p.n : p.rows);
+    const int want = p.tiles_about > 0 ? (WANTED + p.tiles_about - 1) / p.tiles_about : 1;
     p.max_splits = ((p.Kd * (f32 ? 4 : 2) + 127) / 128 + WAVES - 1) / WAVES;
     p.max_splits = p.max_splits < MAX_SPLITS ? p.max_splits : MAX_SPLITS;
-    p.splits = (int)(want < p.max_splits ? want : p.max_splits);
+    p.splits = want < p.max_splits ? want : p.max_splits;
 }
 
 // splits * u_rows <= (WANTED / tiles + 1) * u_rows with tiles >= rows / 64 and, from 1024 rows on, u_rows < 2 * rows: a workspace for

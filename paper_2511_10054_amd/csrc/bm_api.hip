@@ -720,7 +720,7 @@ int check_adapters(const bm_adapter_desc *d) {
 // Scratch of bm_add_adapters: the launch's plan, and its arrays at their places
 struct AdapterLayout {
     AdapterParams p;
-    size_t order, tiles, n_tiles, u, total;
+    size_t order, tiles, u, total;
 };
 
 AdapterLayout make_adapter_layout(const bm_adapter_desc *d) {
@@ -735,7 +735,6 @@ AdapterLayout make_adapter_layout(const bm_adapter_desc *d) {
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes); return o; };
     L.order = take((size_t)p.u_rows * 4);
     L.tiles = take((size_t)p.chunks * p.max_tiles * sizeof(AdapterTile));
-    L.n_tiles = take((size_t)p.chunks * 4);
     L.u = take(adapter_u_rows(p) * p.width * 4);
     L.total = off;
     return L;
@@ -1091,7 +1090,6 @@ int bm_add_adapters(const bm_adapter_desc *desc, const void *x, const int32_t *a
     p.base = base; p.y = y; p.in_place = base == y;
     p.order = at<int32_t>(workspace, L.order);
     p.tiles = at<AdapterTile>(workspace, L.tiles);
-    p.n_tiles = at<int32_t>(workspace, L.n_tiles);
     p.u = at<float>(workspace, L.u);
     return launch_adapters(p, desc->dtype == BM_F32, desc->y_dtype == BM_F32, static_cast<hipStream_t>(stream)) ? BM_ERR_HIP : BM_OK;
 }

@@ -27,6 +27,20 @@ struct F32Line {
     }
 };
 
+// 16 bytes at an address that is a multiple of SIZE bytes
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+template <int SIZE>
+__device__ __forceinline__ u32x4 load_any(const char *at) {
+    if constexpr (SIZE == 4) return *(const BM_GLOBAL u32x4_at4 *)at;
+    else return *(const BM_GLOBAL u32x4_at2 *)at;
+}
+template <int SIZE>
+__device__ __forceinline__ void store_any(char *at, u32x4 v) {
+    if constexpr (SIZE == 4) *(BM_GLOBAL u32x4_at4 *)at = v;
+    else *(BM_GLOBAL u32x4_at2 *)at = v;
+}
+
 // 16 bytes of a row, its values from `at` on (a multiple of 16 bytes), zeros from value `end` on.  WHOLE: the row is at a 16-byte
 // address and holds a multiple of 16 bytes; the values behind `end`, which lie in the row, are read and cleared.
 template <typename L, bool WHOLE>
@@ -44,6 +58,8 @@ __device__ __forceinline__ u32x4 piece(const char *row, int at, int end, int row
                     else v[i / 2] &= i % 2 ? 0x0000ffffu : 0xffff0000u;
                 }
         }
+    } else if (at + PER <= end) {
+        v = load_any<L::SIZE>(row + (size_t)at * L::SIZE);
     } else {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -445,6 +461,8 @@ struct Eight {
             const int at = n + i * PER;
             if constexpr (WHOLE) {
                 v[i] = ldg128(row + (size_t)(at < end ? at : 0) * SIZE);
+            } else if (at + PER <= end) {
+                v[i] = load_any<SIZE>(row + (size_t)at * SIZE);
             } else {
                 v[i] = u32x4{0, 0, 0, 0};
 #pragma unroll
@@ -464,6 +482,8 @@ struct Eight {
             const int at = n + i * PER;
             if constexpr (WHOLE) {
                 if (at < end) stg128(row + (size_t)at * SIZE, v[i]);
+            } else if (at + PER <= end) {
+                store_any<SIZE>(row + (size_t)at * SIZE, v[i]);
             } else {
 #pragma unroll
                 for (int c = 0; c < PER; ++c)

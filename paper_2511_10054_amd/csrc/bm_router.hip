@@ -40,11 +40,16 @@ __device__ __forceinline__ u32x4 piece(const char *row, int at, int bytes) {
         const u32x4 v = ldg128(row + (at < bytes ? at : 0));
         return at < bytes ? v : u32x4{0, 0, 0, 0};
     } else {                               // 4-byte values at any 4-byte address
-        u32x4 v;
+        typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+        u32x4 v = {0, 0, 0, 0};
+        if (at + 16 <= bytes) {
+            v = *(const BM_GLOBAL u32x4_at4 *)(row + at);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int b = at + 4 * i;
-            v[i] = b < bytes ? (uint32_t)ldg_i32(row + b) : 0u;
+            for (int i = 0; i < 3; ++i) {
+                const int b = at + 4 * i;
+                if (b < bytes) v[i] = (uint32_t)ldg_i32(row + b);
+            }
         }
         return v;
     }

@@ -271,6 +271,7 @@ struct FrontEnd {
     bool fuse;
     const int32_t *given_ids;     // the caller's routing: no router, fp.x and fp.wr are not read
     const float *given_w;
+    bool wants_stats;             // the caller asked for them (a routing that is given)
 };
 
 // The caller's routing in place of the router's
@@ -299,7 +300,7 @@ FrontEnd plan_front(const bm_layer_desc *desc, const void *x, const void *w_rout
     f.given_w = given.w;
     f.fuse = !given.ids && front_can_fuse(T, desc->dtype, desc->flags);
     if (!f.fuse && front_wants_logits(fp, desc->dtype) && (size_t)T * E * 4 <= logits_bytes) fp.logits = logits_space;
-    fp.tile_tokens = front_tile_tokens(T, desc->dtype, f.fuse);
+    fp.tile_tokens = given.ids ? TILE_T : front_tile_tokens(T, desc->dtype, f.fuse);
 
     ScanParams &sp = f.sp;
     sp.T = T; sp.E = E; sp.n_shared = desc->n_shared;
@@ -347,8 +348,16 @@ int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, con
         mp.q = fp.q; mp.eta = fp.eta; mp.probs = psi ? at<float>(ws, L.probs) : nullptr;
         mp.ids_in = f.given_ids ? f.given_ids : fp.ids; mp.w_in = f.given_w;
         mp.ids_out = fp.ids2; mp.w = fp.w; mp.stats = sp.stats;
+        if (f.given_ids && remap_groups_ok(T, K, desc->flags)) {
+            ScanParams sq = sp;
+            sq.tile_stats = nullptr;
+            return err | launch_remap_group(mp, sq, cp, st);
+        }
+        const bool counts = !grouping_small((long long)T * K, E);
+        if (f.given_ids && !f.wants_stats) mp.stats = nullptr;
+        if (f.given_ids && counts) mp.tile_counts = fp.tile_counts;      // (its tiles are of TILE_T tokens)
         err |= launch_remap(mp, st);
-        if (!grouping_small((long long)T * K, E)) err |= launch_count(fp.ids2, T, K, E, fp.tile_tokens, fp.tile_counts, st);
+        if (!f.given_ids && counts) err |= launch_count(fp.ids2, T, K, E, fp.tile_tokens, fp.tile_counts, st);
         ScanParams sq = sp;
         sq.tile_stats = nullptr; sq.stats = nullptr;      // written by the substitution kernel
         err |= launch_grouping(sq, cp, st);
@@ -515,6 +524,7 @@ int forward(const bm_layer_desc *desc, const void *x, const bm_weights *wt, cons
         sp.n_mtiles_s = at<int32_t>(ws, L.n_mtiles_s);
     }
     sp.largest_first = per_group ? 1 : 0;
+    fe.wants_stats = dbg && dbg->stats;
     err |= launch_front_end(desc, fe, ws, L, st);
     mark(1);
 
@@ -649,6 +659,7 @@ int forward_quantized(const bm_layer_desc *desc, const void *x, const void *x_q,
         fe.fp.xq = own_q;
         fe.fp.xs = own_s;
     }
+    fe.wants_stats = dbg && dbg->stats;
     err |= launch_front_end(desc, fe, ws, L, st);
     if (!x_q) {
         if (!beside) err |= launch_quantize(x, false, own_q, own_s, 1, T, desc->d, false, st);

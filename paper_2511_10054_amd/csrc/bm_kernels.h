@@ -22,6 +22,7 @@ struct RemapParams {
     int32_t *ids_out;
     float *w;
     const float *w_in;      // [T][K] copied to w first, or null
+    int32_t *tile_counts;   // [E][ceil(T / TILE_T)] histograms of ids_out, or null
     int32_t *stats;         // 6 ints or null
 };
 
@@ -143,6 +144,8 @@ int front_tile_tokens(int T, int dtype, bool fused);   // tokens per workgroup o
 bool front_wants_logits(const FrontParams &p, int dtype);   // FrontParams::logits pays if there is room for it
 int launch_front(const FrontParams &p, int dtype, hipStream_t st);
 int launch_remap(const RemapParams &p, hipStream_t st);
+bool remap_groups_ok(int T, int K, uint32_t flags);   // the batch is small enough for launch_remap_group (which reads w_in)
+int launch_remap_group(const RemapParams &p, const ScanParams &sp, const ScatterParams &cp, hipStream_t st);
 int launch_count(const int32_t *ids, int T, int K, int E, int tile_tokens, int32_t *tile_counts, hipStream_t st);
 int launch_scan(const ScanParams &p, hipStream_t st);
 int launch_scatter(const ScatterParams &p, hipStream_t st);

@@ -350,7 +350,14 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_shrink_kernel(AdapterParam
     __syncthreads();
     f32x4(*sums)[64] = reinterpret_cast<f32x4(*)[64]>(smem);
     if constexpr (WHOLE) {
-        if (tile.count > 16) shrink_ring<L, FEW, NR>(p, tile, rows, blockIdx.y, smem);
+        if (tile.count > 16) {
+            // by the adapter's own rank: what lies behind it is neither loaded nor multiplied
+            const int rank = rank_of(p, tile.adapter);
+            if (NR >= 2 && rank <= 16) shrink_ring<L, FEW, 1>(p, tile, rows, blockIdx.y, smem);
+            else if (NR >= 4 && rank <= 32) shrink_ring<L, FEW, NR >= 2 ? 2 : 1>(p, tile, rows, blockIdx.y, smem);
+            else if (NR >= 8 && rank <= 64) shrink_ring<L, FEW, NR >= 4 ? 4 : 1>(p, tile, rows, blockIdx.y, smem);
+            else shrink_ring<L, FEW, NR>(p, tile, rows, blockIdx.y, smem);
+        }
         else shrink_few<L, true, FEW, NR>(p, tile, rows, blockIdx.y, sums);
     } else {
         // other lengths and addresses: 16 rows at a time
@@ -398,8 +405,8 @@ __device__ __forceinline__ void stage_u(const AdapterParams &p, const TileView &
     constexpr int AHEAD = 4;                                 // (with 8 of them a unit holds fewer waves: 8192 rows 2048 -> 4096 48 -> 52 us)
     constexpr int Q = X::F32 ? 1 : 2;                        // pieces of four ranks: 8 ranks in bf16, 4 in fp32
     const size_t step = (size_t)p.u_rows * p.width;
-    const int blocks = (tile.count + 15) >> 4;
-    for (int at = threadIdx.x; at < X::KB * blocks * 64; at += X::WAVES * 64) {
+    const int blocks = (tile.count + 15) >> 4, kbs = (rank + (X::F32 ? 15 : 31)) / (X::F32 ? 16 : 32);
+    for (int at = threadIdx.x; at < kbs * blocks * 64; at += X::WAVES * 64) {
         const int lane = at & 63, i = (at >> 6) % blocks, kb = (at >> 6) / blocks;
         const int kq = lane >> 4, row = min(i * 16 + (lane & 15), tile.count - 1);
         const int r0 = X::F32 ? kb * 16 + kq * 4 : NR == 1 ? (kq & 1) * 8 : kb * 32 + kq * 8;
@@ -536,7 +543,7 @@ __global__ void __launch_bounds__(expand_waves(NR) * 64) adapter_expand_kernel(A
 #pragma unroll
             for (int kb = 0; kb < X::KB; ++kb) {
                 const int r0 = X::F32 ? kb * 16 + kq * 4 : NR == 1 ? (kq & 1) * 8 : kb * 32 + kq * 8;
-                bv[kb][j] = piece<L, WHOLE>(row, r0, rank, p.rank);
+                if (kb == 0 || kb * (X::F32 ? 16 : 32) < rank) bv[kb][j] = piece<L, WHOLE>(row, r0, rank, p.rank);
             }
         }
     }
@@ -564,13 +571,15 @@ __global__ void __launch_bounds__(expand_waves(NR) * 64) adapter_expand_kernel(A
 #pragma unroll
             for (int j = 0; j < 2 * H; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int kb = 0; kb < X::KB; ++kb)
+            for (int kb = 0; kb < X::KB; ++kb) {
+                if (kb > 0 && kb * (X::F32 ? 16 : 32) >= rank) break;
 #pragma unroll
                 for (int part = 0; part < X::PARTS; ++part) {
                     const u32x4 uv = s.v[part][kb][i][lane];
 #pragma unroll
                     for (int j = 0; j < 2 * H; ++j) acc[j] = L::mac(bv[kb][j], uv, acc[j]);
                 }
+            }
 #pragma unroll
             for (int h = 0; h < H; ++h) v[i][h].add(scale, acc[2 * h], acc[2 * h + 1]);
         }

@@ -91,6 +91,10 @@ CASES = [
     case(1000, 512, 255, 16, 3, 2, 1, "sigmoid", scale=-1.5), case(2049, 1056, 256, 8, 8, 4, 2, "sigmoid"), case(4100, 544, 64, 6, 8, 3, 1),
     case(3000, 96, 8, 2), case(5000, 2048, 128, 8), case(1500, 1443, 60, 4, 5, 3, 2, dtype="f32"), case(1200, 2048, 129, 6, 3, 1, 2, dtype="f32"),
     case(16384 + 37, 64, 66, 3, 2, 1, 2, "sigmoid"),
+    # groups of half a wave; every width and cut of the tiled product: ends of rows inside a line, fewer lines than parts, fp32 too
+    case(70, 128, 256, 5, 2, 1, 2), case(70, 128, 64, 5, 2, 1, 2, "sigmoid"), case(200, 64, 192, 6, 8, 3, 2), case(8200, 96, 256, 8, 8, 4, 2, "sigmoid"),
+    case(4200, 100, 20, 3, dtype="f32"), case(4200, 132, 250, 4, 5, 2, 2, "sigmoid", "f32"), case(900, 4128, 100, 4), case(300, 4160, 250, 4, 2, 1, 1), case(5000, 160, 30, 2),
+    case(2100, 32, 64, 6, 8, 2, 2), case(700, 2052, 90, 4, dtype="f32"), case(5000, 999, 33, 2, dtype="f32"),
 ]
 
 

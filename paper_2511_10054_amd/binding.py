@@ -353,8 +353,8 @@ def bm_workspace_bytes_adapters(desc: AdapterDesc) -> int:
 
 def _rows_ptr(t, stride: int, width: int) -> Optional[int]:
     """Address of a matrix [rows][width] whose rows lie `stride` values apart (0: width)."""
-    if t is None:
-        return None
+    if t is None or (not stride and t.is_contiguous()):
+        return None if t is None else t.data_ptr()
     assert t.dim() == 2 and t.size(1) == width and (t.size(0) < 2 or t.stride(0) == (stride or width)) and (width < 2 or t.stride(1) == 1), \
         "rows must lie as the descriptor says"
     return t.data_ptr()

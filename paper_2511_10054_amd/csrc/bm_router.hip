@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(64) router_small_kernel(RouterParams p) {
 // ---------------------------------------------------------------------------
 #define BM_LDS __attribute__((address_space(3)))
 constexpr int TILE_TOKENS = 128, TILE_WAVES = 8;
+constexpr int LGKM0 = 0xc07f;            // s_waitcnt lgkmcnt(0), the other counters at their most
 
 template <int EB>
 struct RouterTile {
@@ -177,10 +178,13 @@ __global__ void __launch_bounds__(TILE_WAVES * 64, 2) router_tile_kernel(RouterP
             for (int j = 0; j < TN; ++j) acc[i][j] = L::mac(a[h][i], b[h][j], acc[i][j]);
         __builtin_amdgcn_sched_barrier(0);
     };
+    // (The waits for LDS by the builtin, which the compiler knows: left to itself it has every half wait for the other half's reads too.)
     auto line = [&](int l) {
+        __builtin_amdgcn_s_waitcnt(LGKM0);
         read(1);
         multiply(0);
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
+        __builtin_amdgcn_s_waitcnt(LGKM0);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
         load(l + S, now);
         now = now + 1 == S ? 0 : now + 1;
         read(0);

@@ -192,6 +192,11 @@ __device__ __forceinline__ bool find_tile(const AdapterParams &p, int *rows, Til
 template <bool FEW>
 __device__ __forceinline__ size_t place_in_u(const TileView &view, const int *rows, int i) { return FEW ? (size_t)rows[i] : view.place + i; }
 
+__device__ __forceinline__ void wave_lds_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // ---------------------------------------------------------------------------
 // u = A x of a tile and a part of the reduction.  Matrix rows are A's, columns the tile's rows: a lane ends with four neighbouring values
 // of u.  NR: blocks of 16 ranks.
@@ -399,6 +404,30 @@ __device__ __forceinline__ uint32_t take_bf16(float &a, float &b) {
     return v;
 }
 
+// A lane's values of u (eight ranks, four in fp32) in their places
+template <typename L, bool YF32, int NR>
+__device__ __forceinline__ void put_u(float (&v)[8], int kb, int i, int lane, Expanded<L, YF32, NR> &out) {
+    using X = Expanded<L, YF32, NR>;
+    const int kq = lane >> 4;
+    if constexpr (X::F32) {
+        out.v[0][kb][i][lane] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
+    } else {
+        constexpr int VALUES = NR == 1 ? X::PARTS + 1 : X::PARTS;
+        u32x4 part[VALUES];
+#pragma unroll
+        for (int j = 0; j < VALUES; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) part[j][c] = take_bf16(v[2 * c], v[2 * c + 1]);
+        if constexpr (NR == 1) {                             // ranks 0 to 15 twice: the first part, then the second
+            out.v[0][0][i][lane] = kq < 2 ? part[0] : part[1];
+            if constexpr (YF32) out.v[1][0][i][lane] = kq < 2 ? part[2] : u32x4{0, 0, 0, 0};
+        } else {
+#pragma unroll
+            for (int j = 0; j < X::PARTS; ++j) out.v[j][kb][i][lane] = part[j];
+        }
+    }
+}
+
 template <typename L, bool YF32, bool FEW, int NR>
 __device__ __forceinline__ void stage_u(const AdapterParams &p, const TileView &tile, const int *rows, int rank, Expanded<L, YF32, NR> &out) {
     using X = Expanded<L, YF32, NR>;
@@ -436,23 +465,7 @@ __device__ __forceinline__ void stage_u(const AdapterParams &p, const TileView &
         for (int h = 0; h < Q; ++h)
 #pragma unroll
             for (int c = 0; c < 4; ++c) v[4 * h + c] = r0 + 4 * h + c < rank ? sum[h][c] : 0.0f;
-        if constexpr (X::F32) {
-            out.v[0][kb][i][lane] = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
-        } else {
-            constexpr int VALUES = NR == 1 ? X::PARTS + 1 : X::PARTS;
-            u32x4 part[VALUES];
-#pragma unroll
-            for (int j = 0; j < VALUES; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) part[j][c] = take_bf16(v[2 * c], v[2 * c + 1]);
-            if constexpr (NR == 1) {                         // ranks 0 to 15 twice: the first part, then the second
-                out.v[0][0][i][lane] = kq < 2 ? part[0] : part[1];
-                if constexpr (YF32) out.v[1][0][i][lane] = kq < 2 ? part[2] : u32x4{0, 0, 0, 0};
-            } else {
-#pragma unroll
-                for (int j = 0; j < X::PARTS; ++j) out.v[j][kb][i][lane] = part[j];
-            }
-        }
+        put_u<L, YF32, NR>(v, kb, i, lane, out);
     }
 }
 
@@ -590,6 +603,96 @@ __global__ void __launch_bounds__(expand_waves(NR) * 64) adapter_expand_kernel(A
     }
 }
 
+// ---------------------------------------------------------------------------
+// A few rows of a small rank in one launch (one_launch): every workgroup of 256 columns makes u for itself, eight waves every eighth
+// line each.  A is read once for every 256 columns, from the second-level cache; the launch and the round trip of u through memory
+// that this saves take longer (one row 4096 -> 4096, rank 16: 8.2 us in two launches, see one_launch).
+// ---------------------------------------------------------------------------
+constexpr int ONE_WAVES = 8, ONE_ROWS = 16;
+constexpr int ONE_MOST = 16, ONE_BYTES = 128 << 10, ONE_GRID = 256;     // rows; bytes of an adapter's A; workgroups
+static_assert(ONE_MOST <= ONE_ROWS, "a tile's rows");
+
+template <typename L, bool YF32>
+__global__ void __launch_bounds__(ONE_WAVES * 64) adapter_one_kernel(AdapterParams p) {
+    using X = Expanded<L, YF32, 1>;
+    __shared__ X s;
+    __shared__ f32x4 sums[ONE_WAVES][64];
+    __shared__ float u[ONE_ROWS][16];
+    __shared__ int rows[ADAPTER_TILE];
+    TileView tile;
+    if (!find_tile<true>(p, rows, tile)) return;
+    const int lane = lane_id(), wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
+    const bool none = tile.adapter >= p.n;
+    const int rank = none ? 0 : rank_of(p, tile.adapter);
+    const float scale = none || p.scale == nullptr ? 1.0f : ldg_f32(p.scale + tile.adapter);
+    const int n0 = blockIdx.y * RANGE + wave * 32;
+    __syncthreads();
+    const int row = rows[min(r16, tile.count - 1)];
+    Eight<YF32> v;
+    v.template load<true>(static_cast<const char *>(p.base) + (size_t)row * p.base_stride * (YF32 ? 4 : 2), n0 + kq * 8, p.N);
+    if (rank > 0) {
+        u32x4 bv[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const char *at = static_cast<const char *>(p.b) + ((size_t)tile.adapter * p.N + min(n0 + (r16 >> 2) * 8 + j * 4 + (r16 & 3), p.N - 1)) * p.rank * L::SIZE;
+            bv[j] = piece<L, true>(at, X::F32 ? kq * 4 : (kq & 1) * 8, rank, p.rank);
+        }
+        const char *xr = static_cast<const char *>(p.x) + (size_t)row * p.x_stride * L::SIZE;
+        const char *ar = static_cast<const char *>(p.a) + ((size_t)tile.adapter * p.rank + min(r16, p.rank - 1)) * p.Kd * L::SIZE;
+        const int lines = (p.Kd + L::VALUES - 1) / L::VALUES;
+        constexpr int AHEAD = 4;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int l0 = wave; l0 < lines; l0 += ONE_WAVES * AHEAD) {
+            u32x4 xv[AHEAD][2], av[AHEAD][2];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int at = min(l0 + i * ONE_WAVES, lines - 1) * L::VALUES + (h * 4 + kq) * (16 / L::SIZE);
+                    xv[i][h] = piece<L, true>(xr, at, p.Kd, p.Kd);
+                    av[i][h] = piece<L, true>(ar, at, p.Kd, p.Kd);
+                }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (l0 + i * ONE_WAVES >= lines) break;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) acc = L::mac(av[i][h], xv[i][h], acc);
+            }
+        }
+        sums[wave][lane] = acc;
+        __syncthreads();
+        if (wave == 0) {
+            f32x4 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = sums[i][lane] + sums[i + 4][lane];
+            const f32x4 sum = (q[0] + q[1]) + (q[2] + q[3]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) u[r16][kq * 4 + c] = sum[c];
+            wave_lds_fence();
+            float w[8];
+            const int r0 = X::F32 ? kq * 4 : (kq & 1) * 8;
+#pragma unroll
+            for (int c = 0; c < (X::F32 ? 4 : 8); ++c) w[c] = r0 + c < rank ? u[r16][r0 + c] : 0.0f;
+            put_u<L, YF32, 1>(w, 0, 0, lane, s);
+        }
+        __syncthreads();
+        f32x4 d[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int part = 0; part < X::PARTS; ++part)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) d[j] = L::mac(bv[j], s.v[part][0][0][lane], d[j]);
+        v.add(scale, d[0], d[1]);
+    }
+    if (r16 < tile.count) v.template store<true>(static_cast<char *>(p.y) + (size_t)row * p.y_stride * (YF32 ? 4 : 2), n0 + kq * 8, p.N);
+}
+
+// 16 bytes at a time of every array
+bool all_whole(const AdapterParams &p, int size, int ysize) {
+    auto whole = [](const void *q, long long values, int bytes) { return aligned16(q) && values * bytes % 16 == 0; };
+    return whole(p.x, p.x_stride, size) && whole(p.a, p.Kd, size) && whole(p.b, p.rank, size) && whole(p.base, p.base_stride, ysize) &&
+           whole(p.y, p.y_stride, ysize) && p.N * ysize % 16 == 0;
+}
+
 template <typename L, bool FEW, int NR>
 void launch_rank(const AdapterParams &p, bool y_f32, hipStream_t st) {
     auto whole = [](const void *q, long long values, int size) { return aligned16(q) && values * size % 16 == 0; };
@@ -616,6 +719,12 @@ void launch_typed(const AdapterParams &p, bool y_f32, hipStream_t st) {
     else if (p.width <= 32) launch_rank<L, FEW, 2>(p, y_f32, st);
     else if (p.width <= 64) launch_rank<L, FEW, 4>(p, y_f32, st);
     else launch_rank<L, FEW, 8>(p, y_f32, st);
+}
+
+// One launch | two, us: one row 4096 -> 4096 of rank 16 7.5 | 8.2, 16 rows of 16 adapters 8.4 | 9.9, one row 2048 -> 1408 of rank 8
+// 4.6 | 7.5; beyond the limits: one row 8192 -> 4096 (256 KB of A) 11.8 | 9.1, 8 rows 4096 -> 14336 (448 workgroups) 12.9 | 9.4.
+bool one_launch(const AdapterParams &p, bool f32, bool y_f32) {
+    return p.rows <= ONE_MOST && p.rank <= 16 && (long long)p.max_tiles * ((p.N + RANGE - 1) / RANGE) <= ONE_GRID && (long long)p.rank * p.Kd * (f32 ? 4 : 2) <= ONE_BYTES && all_whole(p, f32 ? 4 : 2, y_f32 ? 4 : 2);
 }
 
 }  // namespace
@@ -645,6 +754,13 @@ int launch_adapters(const AdapterParams &p, bool f32, bool y_f32, hipStream_t st
     if (p.rows <= ADAPTER_TILE) {
         AdapterParams few = p;                               // a tile is all rows of an adapter
         few.max_tiles = p.n + (p.in_place ? 0 : 1) < p.rows ? p.n + (p.in_place ? 0 : 1) : p.rows;
+        if (one_launch(few, f32, y_f32)) {
+            const dim3 grid(few.max_tiles, (p.N + RANGE - 1) / RANGE), block(ONE_WAVES * 64);
+            auto one = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, few); };
+            if (f32) y_f32 ? one(adapter_one_kernel<F32Line, true>) : one(adapter_one_kernel<F32Line, false>);
+            else y_f32 ? one(adapter_one_kernel<Bf16Line, true>) : one(adapter_one_kernel<Bf16Line, false>);
+            return launch_status(__func__);
+        }
         if (f32) launch_typed<F32Line, true>(few, y_f32, st);
         else launch_typed<Bf16Line, true>(few, y_f32, st);
         return launch_status(__func__);

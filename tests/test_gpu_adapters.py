@@ -109,6 +109,8 @@ CASES = [
     case(40, 512, 512, 6, 64, "f32", "bf16"), case(300, 128, 256, 3, 128, "f32", "f32", "runs"), case(1, 1, 1, 1, 1, "f32", "f32", none=0.0, ranks=None),
     case(1, 1, 1, 1, 1, none=0.0, ranks=None), case(90, 256, 256, 4, 32, pad=(64, 32, 96)), case(90, 256, 250, 4, 32, y="f32", pad=(3, 5, 1)),
     case(70, 128, 128, 4, 16, shift=1), case(70, 128, 96, 4, 40, "f32", "f32", shift=3, pad=(1, 2, 3)), case(50, 64, 64, 3, 16, none=1.0),
+    case(7, 96, 300, 3, 12, "f32", "f32"), case(16, 128, 264, 5, 16, y="f32"), case(16, 192, 520, 40, 8, none=0.5), case(9, 64, 256, 2, 16, "f32", "bf16", "one"),
+    case(60, 512, 256, 2, 48, order="one", none=0.0), case(64, 300, 256, 2, 128, "f32", "f32", "one"), case(17, 128, 128, 1, 16, none=0.0, pad=(8, 8, 8)),
     case(1200, 64, 128, 4, 16, y="f32", none=0.9), case(600, 2048, 128, 2, 64, order="runs", none=0.0), case(16, 16384, 48, 4, 16),
 ]
 

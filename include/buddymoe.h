@@ -493,8 +493,8 @@ typedef struct {
  * all) is each adapter's own rank, taken as clamped to [0, rank]: values of a and b behind
  * it do not count, whatever they are.  Rows whose adapter lies outside [0, n) get
  * y = base.  base may be y (the same stride): such rows are then neither read nor
- * written; otherwise base, x and y must not overlap.  Rows of a strided array keep what
- * lies between them.
+ * written; otherwise y must not overlap base or x (y == x is refused, BM_ERR_SHAPE).  Rows
+ * of a strided array keep what lies between them.
  * Any sizes, strides and addresses are taken (4-byte addresses in fp32, 2-byte ones in
  * bf16); 16 bytes at a time where rows and addresses are multiples of that.
  * Sums are fp32, a x is held in fp32 (bf16: where b multiplies it, as the sum of three bf16

@@ -1094,7 +1094,7 @@ int bm_add_adapters(const bm_adapter_desc *desc, const void *x, const int32_t *a
     if (!x || !adapter || !a || !b || !base || !y) return BM_ERR_NULL;
     AdapterLayout L = make_adapter_layout(desc);
     AdapterParams &p = L.p;
-    if (base == y && p.base_stride != p.y_stride) return BM_ERR_SHAPE;
+    if (y == x || (base == y && p.base_stride != p.y_stride)) return BM_ERR_SHAPE;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % ALIGN) || workspace_bytes < L.total) return BM_ERR_WORKSPACE;
     (void)hipGetLastError();
     p.x = x; p.adapter = adapter; p.a = a; p.b = b; p.ranks = ranks; p.scale = scale;

@@ -104,9 +104,11 @@ def test_adapters_refuse_pointers():
         args = [None if j == i else ONE for j in range(9)]
         assert lib.bm_add_adapters(ctypes.byref(d), *args, BIG, None) == NULL, i
     for ws, n in ((None, BIG), (ODD, BIG), (ONE, bm.bm_workspace_bytes_adapters(d) - 1)):
-        assert lib.bm_add_adapters(ctypes.byref(d), *(ONE,) * 8, ws, n, None) == WORKSPACE
-    # in place, the rows of base are those of y
-    assert lib.bm_add_adapters(ctypes.byref(_adapters(base_stride=96, y_stride=128)), *(ONE,) * 9, BIG, None) == SHAPE
+        assert lib.bm_add_adapters(ctypes.byref(d), ctypes.c_void_p(512), *(ONE,) * 7, ws, n, None) == WORKSPACE
+    # in place, the rows of base are those of y; x is read while y is written
+    two = ctypes.c_void_p(512)
+    assert lib.bm_add_adapters(ctypes.byref(_adapters(base_stride=96, y_stride=128)), two, *(ONE,) * 8, BIG, None) == SHAPE
+    assert lib.bm_add_adapters(ctypes.byref(d), *(ONE,) * 6, two, ONE, ONE, BIG, None) == SHAPE
     assert lib.bm_add_adapters(None, *(ONE,) * 9, BIG, None) == NULL
     assert lib.bm_workspace_bytes_adapters(None) == 0
     assert lib.bm_add_adapters(ctypes.byref(_adapters(rows=0)), *(None,) * 9, 0, None) == 0

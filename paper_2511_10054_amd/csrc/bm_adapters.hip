@@ -88,7 +88,8 @@ __global__ void __launch_bounds__(ADAPTER_CHUNK) adapter_group_kernel(AdapterPar
     __shared__ int wave_rows[MOST], wave_tiles[MOST];
     const int tid = threadIdx.x, lane = lane_id(), wave = tid >> 6, waves = blockDim.x >> 6, chunk = blockIdx.x;
     const int row = chunk * ADAPTER_CHUNK + tid, keys = p.n + 1;
-    for (int k = tid; k < waves * KEYS; k += blockDim.x) (&count[0][0])[k] = 0;
+    for (int k = tid; k < keys; k += blockDim.x)
+        for (int w = 0; w < waves; ++w) count[w][k] = 0;
     int key = -1;
     if (row < p.rows) {
         key = ldg_i32(p.adapter + row);
@@ -207,25 +208,30 @@ __device__ __forceinline__ void wave_lds_fence() {
 // ---------------------------------------------------------------------------
 #define BM_LDS __attribute__((address_space(3)))
 
-template <typename L, bool WHOLE, bool FEW, int NR>
+template <typename L, bool WHOLE, bool FEW, int NR, int TS>
 __device__ __forceinline__ void shrink_few(const AdapterParams &p, const TileView &tile, const int *rows, int split, f32x4 (*sums)[64]) {
     const int lane = lane_id(), wave = threadIdx.x >> 6, r16 = lane & 15, kq = lane >> 4;
     const int lines = (p.Kd + L::VALUES - 1) / L::VALUES;
     const int begin = (int)((long long)split * lines / p.splits), end = (int)((long long)(split + 1) * lines / p.splits);
     const int blocks = (rank_of(p, tile.adapter) + 15) >> 4;                  // of ranks that count
-    const char *xr = static_cast<const char *>(p.x) + (size_t)rows[min(r16, tile.count - 1)] * p.x_stride * L::SIZE, *ar[NR];
+    const char *xr[TS], *ar[NR];
+#pragma unroll
+    for (int i = 0; i < TS; ++i) xr[i] = static_cast<const char *>(p.x) + (size_t)rows[min(i * 16 + r16, tile.count - 1)] * p.x_stride * L::SIZE;
 #pragma unroll
     for (int j = 0; j < NR; ++j)
         ar[j] = static_cast<const char *>(p.a) + ((size_t)tile.adapter * p.rank + min(j * 16 + r16, p.rank - 1)) * p.Kd * L::SIZE;
-    f32x4 acc[NR];
+    f32x4 acc[NR][TS];
 #pragma unroll
-    for (int j = 0; j < NR; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NR; ++j)
+#pragma unroll
+        for (int i = 0; i < TS; ++i) acc[j][i] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int l = begin + wave; l < end; l += WAVES) {
-        u32x4 xv[2], av[NR][2];
+        u32x4 xv[TS][2], av[NR][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = l * L::VALUES + (h * 4 + kq) * (16 / L::SIZE);
-            xv[h] = piece<L, WHOLE>(xr, at, p.Kd, p.Kd);
+#pragma unroll
+            for (int i = 0; i < TS; ++i) xv[i][h] = piece<L, WHOLE>(xr[i], at, p.Kd, p.Kd);
 #pragma unroll
             for (int j = 0; j < NR; ++j)
                 if (j < blocks) av[j][h] = piece<L, WHOLE>(ar[j], at, p.Kd, p.Kd);
@@ -234,27 +240,37 @@ __device__ __forceinline__ void shrink_few(const AdapterParams &p, const TileVie
         for (int j = 0; j < NR; ++j) {
             if (j >= blocks) break;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) acc[j] = L::mac(av[j][h], xv[h], acc[j]);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < TS; ++i) acc[j][i] = L::mac(av[j][h], xv[i][h], acc[j][i]);
         }
     }
     if (wave >= 2)
 #pragma unroll
-        for (int j = 0; j < NR; ++j) sums[(wave - 2) * NR + j][lane] = acc[j];
+        for (int j = 0; j < NR; ++j)
+#pragma unroll
+            for (int i = 0; i < TS; ++i) sums[((wave - 2) * NR + j) * TS + i][lane] = acc[j][i];
     __syncthreads();
     if (wave < 2)
 #pragma unroll
-        for (int j = 0; j < NR; ++j) {
-            f32x4 &other = sums[wave * NR + j][lane];
-            acc[j] += other;
-            if (wave == 1) other = acc[j];
-        }
-    __syncthreads();
-    if (wave != 0 || r16 >= tile.count) return;
-    float *u = p.u + (split * (size_t)p.u_rows + place_in_u<FEW>(tile, rows, r16)) * p.width;
+        for (int j = 0; j < NR; ++j)
 #pragma unroll
-    for (int j = 0; j < NR; ++j) {
-        if (j >= blocks) break;
-        *(BM_GLOBAL f32x4 *)(u + j * 16 + kq * 4) = acc[j] + sums[NR + j][lane];
+            for (int i = 0; i < TS; ++i) {
+                f32x4 &other = sums[(wave * NR + j) * TS + i][lane];
+                acc[j][i] += other;
+                if (wave == 1) other = acc[j][i];
+            }
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 0; i < TS; ++i) {
+        if (i * 16 + r16 >= tile.count) continue;
+        float *u = p.u + (split * (size_t)p.u_rows + place_in_u<FEW>(tile, rows, i * 16 + r16)) * p.width;
+#pragma unroll
+        for (int j = 0; j < NR; ++j) {
+            if (j >= blocks) break;
+            *(BM_GLOBAL f32x4 *)(u + j * 16 + kq * 4) = acc[j][i] + sums[(NR + j) * TS + i][lane];
+        }
     }
 }
 
@@ -347,7 +363,8 @@ __device__ __forceinline__ void shrink_ring(const AdapterParams &p, const TileVi
 template <typename L, bool WHOLE, bool FEW, int NR>
 __global__ void __launch_bounds__(WAVES * 64) adapter_shrink_kernel(AdapterParams p) {
     using R = Ring<NR>;
-    __shared__ u32x4 smem[WHOLE ? R::STAGES * R::STAGE : 2 * NR * 64];
+    constexpr int TS = WHOLE || NR >= 8 ? 1 : NR >= 4 ? 2 : ADAPTER_TILE / 16;               // blocks of 16 rows at a time straight from memory
+    __shared__ u32x4 smem[WHOLE ? R::STAGES * R::STAGE : 2 * NR * TS * 64];
     static_assert(R::STAGES * R::STAGE >= 2 * NR * 64, "holds the waves' sums of up to 16 rows");
     __shared__ int rows[ADAPTER_TILE];
     TileView tile;
@@ -363,12 +380,12 @@ __global__ void __launch_bounds__(WAVES * 64) adapter_shrink_kernel(AdapterParam
             else if (NR >= 8 && rank <= 64) shrink_ring<L, FEW, NR >= 4 ? 4 : 1>(p, tile, rows, blockIdx.y, smem);
             else shrink_ring<L, FEW, NR>(p, tile, rows, blockIdx.y, smem);
         }
-        else shrink_few<L, true, FEW, NR>(p, tile, rows, blockIdx.y, sums);
+        else shrink_few<L, true, FEW, NR, 1>(p, tile, rows, blockIdx.y, sums);
     } else {
-        // other lengths and addresses: 16 rows at a time
-        for (int i = 0; i < tile.count; i += 16) {
-            TileView part{tile.adapter, min(16, tile.count - i), tile.place + i};
-            shrink_few<L, false, FEW, NR>(p, part, rows + i, blockIdx.y, sums);
+        // other lengths and addresses
+        for (int i = 0; i < tile.count; i += 16 * TS) {
+            TileView part{tile.adapter, min(16 * TS, tile.count - i), tile.place + i};
+            shrink_few<L, false, FEW, NR, TS>(p, part, rows + i, blockIdx.y, sums);
             __syncthreads();
         }
     }

@@ -498,8 +498,9 @@ typedef struct {
  * Any sizes, strides and addresses are taken (4-byte addresses in fp32, 2-byte ones in
  * bf16); 16 bytes at a time where rows and addresses are multiples of that.
  * Sums are fp32, a x is held in fp32 (bf16: where b multiplies it, as the sum of three bf16
- * values, its 24 bits, or for a bf16 y of two); y is rounded once.  Equal calls give equal
- * bits; a row's y can differ in its last bits with the rest of the batch.
+ * values, its 24 bits, or for a bf16 y of two; an infinity in b then gives infinities or
+ * NaN); y is rounded once.  Equal calls give equal bits; a row's y can differ in its last
+ * bits with the rest of the batch.
  * workspace: device scratch, 256-byte aligned, of at least
  * bm_workspace_bytes_adapters(desc) bytes.  rows == 0 is a no-op. */
 int bm_add_adapters(const bm_adapter_desc *desc, const void *x, const int32_t *adapter, const void *a,

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(TILE_WAVES * 64, 2) router_tile_kernel(RouterP
         read(1);
         multiply(0);
         __builtin_amdgcn_s_waitcnt(LGKM0);
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((S - 2) * R::LOADS) : "memory");
         load(l + S, now);
         now = now + 1 == S ? 0 : now + 1;
         read(0);

@@ -53,6 +53,13 @@ def test_same_bits_as_the_layer_that_routes(name, over, T, kw):
     for k in ("ids", "ids_remapped", "offsets", "perm", "inv_perm"):
         np.testing.assert_array_equal(dbg[k].cpu().numpy(), np.asarray(want[k]).reshape(-1), err_msg=k)
     np.testing.assert_array_equal(dbg["w"].cpu().numpy(), np.asarray(want["w"]).reshape(-1))
+    np.testing.assert_array_equal(dbg["stats"].cpu().numpy(), np.asarray(want["stats"]))
+    # without the intermediate arrays (whose counters then are not kept), and in a workspace that holds something else: the same bits
+    for fill in (255, 1):
+        dev.workspace.fill_(fill)
+        y.fill_(float("nan"))
+        bm.bm_moe_forward_routed(dev.desc, dev.x, ids, w, no_router, dev.bitmap, dev.table, y, dev.workspace)
+        np.testing.assert_array_equal(y.float().cpu().numpy(), want["y"])
 
 
 def test_ids_outside_and_ids_twice():

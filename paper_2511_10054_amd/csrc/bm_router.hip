@@ -296,18 +296,26 @@ __device__ __forceinline__ int better_groups(const RouterParams &p, const Two &t
     return better;
 }
 
-// The lane's value v of EC, from a row of n values at a 4-byte address; whole: n is a multiple of EC and the row is at a multiple of
-// EC values
-template <int EC>
-__device__ __forceinline__ void load_lane(const float *row, int lane, int n, bool whole, float (&v)[EC]) {
-    if (EC == 4 && whole) {
-        const f32x4 q = *(const BM_GLOBAL f32x4 *)(row + min(lane * 4, n - 4));
+// The lane's EC values of each part of a token's logits, of the bias and of the balance.  One branch for all of the loads: with one for
+// each array the compiler has a load wait for those before.
+template <int EC, int N, bool WHOLE>
+__device__ __forceinline__ void load_lane(const RouterParams &p, int t, int lane, float (&part)[N][EC], float (&bias)[EC], float (&balance)[EC]) {
+    const int E = p.E;
+    const float *z = p.logits + (size_t)t * E;
+    auto load = [&](const float *row, float (&v)[EC]) {
+        if constexpr (WHOLE) {             // E is a multiple of 4, and rows are at 16-byte addresses
+            const f32x4 q = *(const BM_GLOBAL f32x4 *)(row + min(lane * 4, E - 4));
 #pragma unroll
-        for (int i = 0; i < EC; ++i) v[i] = q[i % 4];
-    } else {
+            for (int i = 0; i < EC; ++i) v[i] = q[i % 4];
+        } else {
 #pragma unroll
-        for (int i = 0; i < EC; ++i) v[i] = ldg_f32(row + min(lane * EC + i, n - 1));
-    }
+            for (int i = 0; i < EC; ++i) v[i] = ldg_f32(row + min(lane * EC + i, E - 1));
+        }
+    };
+#pragma unroll
+    for (int n = 0; n < N; ++n) load(z + (size_t)n * p.T * E, part[n]);
+    load(p.bias != nullptr ? p.bias : z, bias);            // (of none: values that are not used)
+    load(p.balance != nullptr ? p.balance : z, balance);
 }
 
 template <int EC, int N>
@@ -317,14 +325,14 @@ __global__ void __launch_bounds__(SELECT_WAVES * 64) select_kernel(RouterParams 
     if (t >= p.T) return;
     const float NEVER = -__builtin_inff();
     const int E = p.E;
-    const bool whole = E % 4 == 0;
     float part[N][EC], s[EC], c[EC];
+    if (EC == 4 && E % 4 == 0 && aligned16(p.bias) && aligned16(p.balance)) load_lane<EC, N, EC == 4>(p, t, lane, part, s, c);
+    else load_lane<EC, N, false>(p, t, lane, part, s, c);
 #pragma unroll
-    for (int n = 0; n < N; ++n) load_lane<EC>(p.logits + ((size_t)n * p.T + t) * E, lane, E, whole, part[n]);
-#pragma unroll
-    for (int i = 0; i < EC; ++i) s[i] = c[i] = 0.0f;
-    if (p.bias != nullptr) load_lane<EC>(p.bias, lane, E, whole && aligned16(p.bias), s);
-    if (p.balance != nullptr) load_lane<EC>(p.balance, lane, E, whole && aligned16(p.balance), c);
+    for (int i = 0; i < EC; ++i) {
+        s[i] = p.bias != nullptr ? s[i] : 0.0f;
+        c[i] = p.balance != nullptr ? c[i] : 0.0f;
+    }
 #pragma unroll
     for (int i = 0; i < EC; ++i) {
         float q[4];

@@ -351,19 +351,26 @@ def bm_workspace_bytes_adapters(desc: AdapterDesc) -> int:
     return int(load_library().bm_workspace_bytes_adapters(ctypes.byref(desc)))
 
 
-def _rows_ptr(t, stride: int, width: int) -> Optional[int]:
-    """Address of a matrix [rows][width] whose rows lie `stride` values apart (0: width)."""
-    if t is None or (not stride and t.is_contiguous()):
-        return None if t is None else t.data_ptr()
-    assert t.dim() == 2 and t.size(1) == width and (t.size(0) < 2 or t.stride(0) == (stride or width)) and (width < 2 or t.stride(1) == 1), \
-        "rows must lie as the descriptor says"
+def _rows_ptr(t, stride: int, width: int, rows: int) -> Optional[int]:
+    """Address of a matrix [rows][width] whose rows lie `stride` values apart (0: width); a contiguous one may have any leading dimensions."""
+    if t is None:
+        return None
+    shape = t.shape                                     # (once: a look at it costs more than the comparisons)
+    if not stride and t.is_contiguous():
+        if len(shape) == 2 and shape[1] == width and shape[0] >= rows:
+            return t.data_ptr()
+        lies = (len(shape) < 2 or shape[-1] == width) and t.numel() >= rows * width
+    else:
+        lies = len(shape) == 2 and shape[0] >= rows and shape[1] == width and \
+            (shape[0] < 2 or t.stride(0) == (stride or width)) and (width < 2 or t.stride(1) == 1)
+    assert lies, "rows must lie as the descriptor says"
     return t.data_ptr()
 
 
 def bm_add_adapters(desc: AdapterDesc, x, adapter, a, b, ranks, scale, base, y, workspace, stream: Optional[int] = None):
     """y = base + scale[s] * b[s] (a[s] x) with s = adapter[row]; x, base and y may be columns of wider matrices (desc's strides)."""
-    _check(load_library().bm_add_adapters(ctypes.byref(desc), _rows_ptr(x, desc.x_stride, desc.Kd), _ptr(adapter), _ptr(a), _ptr(b),
-                                          _ptr(ranks), _ptr(scale), _rows_ptr(base, desc.base_stride, desc.N),
-                                          _rows_ptr(y, desc.y_stride, desc.N), _ptr(workspace),
+    _check(load_library().bm_add_adapters(ctypes.byref(desc), _rows_ptr(x, desc.x_stride, desc.Kd, desc.rows), _ptr(adapter), _ptr(a), _ptr(b),
+                                          _ptr(ranks), _ptr(scale), _rows_ptr(base, desc.base_stride, desc.N, desc.rows),
+                                          _rows_ptr(y, desc.y_stride, desc.N, desc.rows), _ptr(workspace),
                                           workspace.numel() * workspace.element_size(),
                                           _stream() if stream is None else stream), "bm_add_adapters")

@@ -184,6 +184,7 @@ int check_moe_args(const bm_layer_desc *desc, const void *x, const bm_weights *w
     if (rc) return rc;
     rc = check_remap_desc(desc);
     if (rc) return rc;
+    if (given_routing && (desc->flags & BM_PSI_TOKEN)) return BM_ERR_SHAPE;     // needs the router's probabilities
     if (desc->T == 0) return BM_OK;
     if (!x || !wt || !residency_bitmap || !y || (!buddy_table && desc->R > 0)) return BM_ERR_NULL;
     if ((!wt->w_router && !given_routing) || !wt->w_gate || !wt->w_up || !wt->w_down) return BM_ERR_NULL;
@@ -965,9 +966,7 @@ int bm_moe_forward_routed(const bm_layer_desc *desc, const void *x, const int32_
                           const uint64_t *residency_bitmap, const int32_t *buddy_table, void *y, void *workspace,
                           size_t workspace_bytes, const bm_debug_out *dbg, void *stream) {
     const int rc = check_moe_args(desc, x, wt, residency_bitmap, buddy_table, y, true);
-    if (rc) return rc;
-    if (desc->flags & BM_PSI_TOKEN) return BM_ERR_SHAPE;      // needs the router's probabilities
-    if (desc->T == 0) return BM_OK;
+    if (rc || desc->T == 0) return rc;
     if (!ids || !w) return BM_ERR_NULL;
     return forward(desc, x, wt, GivenRouting{ids, w}, residency_bitmap, buddy_table, y, workspace, workspace_bytes, dbg, stream);
 }

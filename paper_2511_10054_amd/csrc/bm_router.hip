@@ -269,11 +269,12 @@ __device__ __forceinline__ float row_sum(float v) {
     return read_lane(v, 63);
 }
 
-// e^x: 2^(x log2 e) with the rest of the product, which the instruction's argument has no room for
+// e^x: 2^(x log2 e) with the rest of the product, which the instruction's argument has no room for (at 87 up to 63 * 2^-24 of the result).
+// From 128 on the instruction gives infinity, or zero, and the rest of an infinity is no number.
 __device__ __forceinline__ float exponential(float x) {
     const float hi = x * 0x1.715476p+0f, lo = fmaf(x, 0x1.715476p+0f, -hi) + x * 0x1.4ae0c0p-26f;    // log2 e in two parts
     const float e = __builtin_amdgcn_exp2f(hi);
-    return fabsf(hi) < 120.0f ? fmaf(e, lo * 0x1.62e430p-1f, e) : e;                                 // 2^lo = 1 + lo log 2
+    return fabsf(hi) < 128.0f ? fmaf(e, lo * 0x1.62e430p-1f, e) : e;                                 // 2^lo = 1 + lo log 2
 }
 
 struct Two {                               // the largest and second largest of a set

@@ -414,12 +414,15 @@ struct Expanded {
     u32x4 v[PARTS][KB][ADAPTER_TILE / 16][64];
 };
 
-// The bf16 values of a pair, and what they leave of it (an infinity leaves nothing)
+// The bf16 values of a pair, and what they leave of it.  The largest number of bf16 is below fp32's: what lies above it, infinities and
+// what is no number leave the rest to the last part, which is rounded as it comes.
+template <bool LAST>
 __device__ __forceinline__ uint32_t take_bf16(float &a, float &b) {
-    const uint32_t v = pack_bf16x2(a, b);
-    const float x = __builtin_bit_cast(float, v << 16), y = __builtin_bit_cast(float, v & 0xffff0000u);
-    a = fabsf(x) < __builtin_inff() ? a - x : 0.0f;
-    b = fabsf(y) < __builtin_inff() ? b - y : 0.0f;
+    if constexpr (LAST) return pack_bf16x2(a, b);
+    constexpr float MOST = 0x1.fep127f;
+    const uint32_t v = pack_bf16x2(__builtin_amdgcn_fmed3f(a, -MOST, MOST), __builtin_amdgcn_fmed3f(b, -MOST, MOST));
+    a -= __builtin_bit_cast(float, v << 16);
+    b -= __builtin_bit_cast(float, v & 0xffff0000u);
     return v;
 }
 
@@ -436,7 +439,7 @@ __device__ __forceinline__ void put_u(float (&v)[8], int kb, int i, int lane, Ex
 #pragma unroll
         for (int j = 0; j < VALUES; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) part[j][c] = take_bf16(v[2 * c], v[2 * c + 1]);
+            for (int c = 0; c < 4; ++c) part[j][c] = j + 1 < VALUES ? take_bf16<false>(v[2 * c], v[2 * c + 1]) : take_bf16<true>(v[2 * c], v[2 * c + 1]);
         if constexpr (NR == 1) {                             // ranks 0 to 15 twice: the first part, then the second
             out.v[0][0][i][lane] = kq < 2 ? part[0] : part[1];
             if constexpr (YF32) out.v[1][0][i][lane] = kq < 2 ? part[2] : u32x4{0, 0, 0, 0};

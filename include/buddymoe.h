@@ -440,13 +440,17 @@ typedef struct {
 /* Routing by scores, with a bias for balance and groups of experts:
  *   z[t][e] = bias[e] + sum_j x[t][j] * w_router[e][j]      (fp32 accumulation)
  *   s = softmax(z) over all E, or 1 / (1 + exp(-z));   c = s + balance[e]
- * A group's score is the sum of its group_top largest c; the keep_groups groups of
- * largest score stay, equal scores the lower group.  ids[t][0..K) = the K experts of
+ * A group's score is the sum of its group_top largest c (-infinity where that is no
+ * number: an infinite c and one of -infinity); the keep_groups groups of largest
+ * score stay, equal scores the lower group.  ids[t][0..K) = the K experts of
  * largest c in them, slot 0 the largest, equal c to the lower index; w[t][k] = s of
  * slot k, without the balance, with BM_RENORM_TOPK divided by the K slots' sum (by
  * 2^-126 where that is larger), times scale.  An expert whose c is -infinity or NaN
  * is never chosen (a balance of -infinity switches it off): slots without an
  * expert get id -1 and w 0, which bm_buddy_remap and the layer drop.
+ * s and c are fp32, s off by a few units in the last place: experts whose c comes to the same
+ * fp32 value are equal and go by index (all sigmoids of z above 17.4 are 1), and an
+ * s below 2^-126 may be 0.
  * x [T][d], w_router [E][d] (bf16: 16-byte aligned, BM_ERR_ALIGN otherwise), bias and
  * balance [E] fp32 or NULL, ids [T][K] int32 and w [T][K] fp32 (written), all device.
  * A token's ids and w are the same bits whatever T it is part of.  workspace: device
@@ -461,6 +465,8 @@ size_t bm_workspace_bytes_scored(const bm_router_desc *desc);   /* host; 0 if de
  * substitution, grouping, experts and aggregation, with the same gates (they read the
  * weights renormalised to sum 1), workspace and results.  ids [T][K] int32, w [T][K] fp32
  * (device, not written; ids outside [0,E) are dropped, one listed twice counts twice).
+ * In bf16 h and, past decode sizes, o are held in bf16, as in bm_moe_forward: up to three
+ * roundings to bf16 on the way to y in place of one; the 8-bit layer's h is held in e4m3.
  * w_router and router_bias of the weights are not read and may be NULL, nor is x of the
  * 8-bit layer when x_q is given.  BM_RENORM_TOPK is not read.  BM_PSI_TOKEN needs the
  * router's probabilities and is refused (BM_ERR_SHAPE).  dbg->ids gets ids as given. */

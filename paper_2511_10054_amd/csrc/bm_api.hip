@@ -333,8 +333,10 @@ int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, con
         fp.scat = cp;
         err |= launch_front(fp, desc->dtype, st);
     } else if (f.given_ids || (desc->flags & BM_GATE_DIST)) {
-        // the distribution gate needs every token's routing before the first substitution: route,
-        // then substitute (each workgroup derives the batch's request set itself), then count
+        // A routing that is given has no router to be fused with: substitution and grouping of up to 64 tokens of at most 1024 slots without the
+        // distribution gate in one launch; else substitution, which leaves the histograms where the grouping starts from them.
+        // The distribution gate needs every token's routing before the first substitution: route,
+        // then substitute (each workgroup derives the batch's request set itself), then count.
         const bool psi = (desc->flags & BM_PSI_TOKEN) != 0;
         if (!f.given_ids) {
             FrontParams rp = fp;
@@ -342,7 +344,7 @@ int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, con
             if (psi) rp.probs_out = at<float>(ws, L.probs);
             err |= launch_front(rp, desc->dtype, st);
         }
-        RemapParams mp{};
+        GivenRemapParams mp{};
         mp.T = T; mp.K = K; mp.E = E; mp.R = desc->R; mp.H = desc->H;
         mp.flags = desc->flags; mp.tau = fp.tau; mp.gamma = fp.gamma; mp.rho = fp.rho; mp.beta = fp.beta;
         mp.bitmap = fp.bitmap; mp.table = fp.table;
@@ -357,7 +359,7 @@ int launch_front_end(const bm_layer_desc *desc, const FrontEnd &f, void *ws, con
         const bool counts = !grouping_small((long long)T * K, E);
         if (f.given_ids && !f.wants_stats) mp.stats = nullptr;
         if (f.given_ids && counts) mp.tile_counts = fp.tile_counts;      // (its tiles are of TILE_T tokens)
-        err |= launch_remap(mp, st);
+        err |= f.given_ids ? launch_remap(mp, st) : launch_remap(static_cast<const RemapParams &>(mp), st);
         if (!f.given_ids && counts) err |= launch_count(fp.ids2, T, K, E, fp.tile_tokens, fp.tile_counts, st);
         ScanParams sq = sp;
         sq.tile_stats = nullptr; sq.stats = nullptr;      // written by the substitution kernel

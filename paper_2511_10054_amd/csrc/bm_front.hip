@@ -1347,15 +1347,18 @@ __global__ void __launch_bounds__(NW * 64) front_f32_kernel(FrontParams p) {
 // grid-wide wait): 16 bytes per load, eight loads in flight per lane (3001 tokens of 8 out of 128 experts: 8.8 us; 62 us
 // with one 4-byte load in flight, the buddy rows scanned entry by entry and a whole walk per lane).
 // A single workgroup stores the counters, several add theirs to zeros (launch_remap).
+// GIVEN: in front of a layer on a routing that the caller has, whose weights are copied and whose histograms the grouping may want.  A
+// kernel and parameters of its own: with a branch in the same one bm_buddy_remap took 0.1 to 0.4 us more (3001 tokens behind the
+// distribution gate 8.67 | 9.05 us, 64 tokens 6.64 | 6.80).
 // ---------------------------------------------------------------------------
-template <int W, int KC = 0>        // KC = 1: one slot per token, else p.K
-__global__ void __launch_bounds__(1024) remap_kernel(RemapParams p) {
+template <int W, int KC = 0, bool GIVEN = false>        // KC = 1: one slot per token, else p.K
+__global__ void __launch_bounds__(1024) remap_kernel(std::conditional_t<GIVEN, GivenRemapParams, RemapParams> p) {
     extern __shared__ int32_t s_table[];                // E * R entries, then E acceptable-entry masks
     __shared__ int32_t s_req[64 * W];                   // distribution gate: the expert was routed to
     __shared__ int32_t s_ids[REMAP_TOK * BM_MAX_K];
     __shared__ unsigned long long s_used[REMAP_TOK * W];
     __shared__ int32_t s_stats[3];
-    __shared__ int32_t s_counts[2 * 64 * W];
+    __shared__ int32_t s_counts[GIVEN ? 2 * 64 * W : 1];
     static_assert(REMAP_TOK == 2 * TILE_T, "two histograms a tile");
     const int tid = threadIdx.x;
     const int ec = (p.E + 63) >> 6;
@@ -1418,7 +1421,7 @@ __global__ void __launch_bounds__(1024) remap_kernel(RemapParams p) {
             for (int idx = tid; idx < n; idx += blockDim.x) s_ids[idx] = in[idx];
             __syncthreads();
         }
-        if (p.w_in != nullptr) {
+        if constexpr (GIVEN) {
             for (int idx = tid; idx < n; idx += blockDim.x) p.w[(size_t)t0 * p.K + idx] = p.w_in[(size_t)t0 * p.K + idx];
             __syncthreads();
         }
@@ -1427,16 +1430,18 @@ __global__ void __launch_bounds__(1024) remap_kernel(RemapParams p) {
         remap_tile<W, KC>(ntok, p.K, p.E, p.R, p.flags, p.tau, p.gamma, p.rho, resident, accept, s_table, s_ids,
                       p.w != nullptr ? p.w + (size_t)t0 * p.K : nullptr, s_used, s_stats, psi);
         for (int idx = tid; idx < n; idx += blockDim.x) p.ids_out[(size_t)t0 * p.K + idx] = s_ids[idx];
-        if (p.tile_counts != nullptr) {                  // the histograms that the grouping starts from, of TILE_T tokens each
-            for (int e = tid; e < 2 * 64 * W; e += blockDim.x) s_counts[e] = 0;
-            __syncthreads();
-            for (int idx = tid; idx < n; idx += blockDim.x)
-                if (s_ids[idx] >= 0) atomicAdd(&s_counts[(idx >= TILE_T * p.K ? 64 * W : 0) + s_ids[idx]], 1);
-            __syncthreads();
-            const int tiles = (p.T + TILE_T - 1) / TILE_T, tile = t0 / TILE_T;
-            for (int e = tid; e < p.E; e += blockDim.x) {
-                p.tile_counts[(size_t)e * tiles + tile] = s_counts[e];
-                if (tile + 1 < tiles) p.tile_counts[(size_t)e * tiles + tile + 1] = s_counts[64 * W + e];
+        if constexpr (GIVEN) {
+            if (p.tile_counts != nullptr) {                  // the histograms that the grouping starts from, of TILE_T tokens each
+                for (int e = tid; e < 2 * 64 * W; e += blockDim.x) s_counts[e] = 0;
+                __syncthreads();
+                for (int idx = tid; idx < n; idx += blockDim.x)
+                    if (s_ids[idx] >= 0) atomicAdd(&s_counts[(idx >= TILE_T * p.K ? 64 * W : 0) + s_ids[idx]], 1);
+                __syncthreads();
+                const int tiles = (p.T + TILE_T - 1) / TILE_T, tile = t0 / TILE_T;
+                for (int e = tid; e < p.E; e += blockDim.x) {
+                    p.tile_counts[(size_t)e * tiles + tile] = s_counts[e];
+                    if (tile + 1 < tiles) p.tile_counts[(size_t)e * tiles + tile + 1] = s_counts[64 * W + e];
+                }
             }
         }
         __syncthreads();
@@ -1748,7 +1753,7 @@ __global__ void __launch_bounds__(1024) group_small_kernel(ScanParams p, Scatter
 // A small batch whose routing is given (remap_groups_ok): substitution and grouping in one workgroup, 3 us less than in two launches.
 // ---------------------------------------------------------------------------
 template <int W>
-__global__ void __launch_bounds__(1024) remap_group_kernel(RemapParams p, ScanParams sp, ScatterParams cp) {
+__global__ void __launch_bounds__(1024) remap_group_kernel(GivenRemapParams p, ScanParams sp, ScatterParams cp) {
     extern __shared__ int32_t s_table[];                // E * R entries, then E acceptable-entry masks
     __shared__ int32_t s_ids[SMALL_ANY];
     __shared__ unsigned long long s_used[REMAP_TOK * W];
@@ -1860,7 +1865,8 @@ int launch_front(const FrontParams &p, int dtype, hipStream_t st) {
     return launch_status(__func__);
 }
 
-int launch_remap(const RemapParams &p, hipStream_t st) {
+template <bool GIVEN, typename Params>
+static int launch_remap_kernel(const Params &p, hipStream_t st) {
     if (p.T <= 0) {
         if (p.stats) hipLaunchKernelGGL(zero_ints_kernel, dim3(1), dim3(64), 0, st, p.stats, 6);
         return launch_status(__func__);
@@ -1878,8 +1884,8 @@ int launch_remap(const RemapParams &p, hipStream_t st) {
     }
 #define BM_REMAP(W_)                                                                                           \
     {                                                                                                          \
-        if (p.K == 1) hipLaunchKernelGGL((remap_kernel<W_, 1>), dim3(blocks), dim3(threads), lds, st, p);      \
-        else hipLaunchKernelGGL((remap_kernel<W_>), dim3(blocks), dim3(threads), lds, st, p);                  \
+        if (p.K == 1) hipLaunchKernelGGL((remap_kernel<W_, 1, GIVEN>), dim3(blocks), dim3(threads), lds, st, p); \
+        else hipLaunchKernelGGL((remap_kernel<W_, 0, GIVEN>), dim3(blocks), dim3(threads), lds, st, p);          \
     }
     if (p.E <= 64) BM_REMAP(1)
     else if (p.E <= 128) BM_REMAP(2)
@@ -1888,11 +1894,14 @@ int launch_remap(const RemapParams &p, hipStream_t st) {
     return launch_status(__func__);
 }
 
+int launch_remap(const RemapParams &p, hipStream_t st) { return launch_remap_kernel<false>(p, st); }
+int launch_remap(const GivenRemapParams &p, hipStream_t st) { return launch_remap_kernel<true>(p, st); }
+
 bool remap_groups_ok(int T, int K, uint32_t flags) {
     return T > 0 && T <= REMAP_TOK && T * K <= SMALL_ANY && !(flags & (BM_GATE_DIST | BM_PSI_TOKEN));
 }
 
-int launch_remap_group(const RemapParams &p, const ScanParams &sp, const ScatterParams &cp, hipStream_t st) {
+int launch_remap_group(const GivenRemapParams &p, const ScanParams &sp, const ScatterParams &cp, hipStream_t st) {
     const size_t lds = (size_t)p.E * (p.R + 1) * sizeof(int32_t);
     if (p.E <= 64) hipLaunchKernelGGL(remap_group_kernel<1>, dim3(1), dim3(1024), lds, st, p, sp, cp);
     else if (p.E <= 128) hipLaunchKernelGGL(remap_group_kernel<2>, dim3(1), dim3(1024), lds, st, p, sp, cp);

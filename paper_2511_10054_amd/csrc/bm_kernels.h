@@ -21,9 +21,13 @@ struct RemapParams {
     const int32_t *ids_in;
     int32_t *ids_out;
     float *w;
-    const float *w_in;      // [T][K] copied to w first, or null
-    int32_t *tile_counts;   // [E][ceil(T / TILE_T)] histograms of ids_out, or null
     int32_t *stats;         // 6 ints or null
+};
+
+// In front of a layer on a routing that the caller has
+struct GivenRemapParams : RemapParams {
+    const float *w_in;      // [T][K] copied to w first
+    int32_t *tile_counts;   // [E][ceil(T / TILE_T)] histograms of ids_out, or null
 };
 
 struct ScanParams {
@@ -144,8 +148,9 @@ int front_tile_tokens(int T, int dtype, bool fused);   // tokens per workgroup o
 bool front_wants_logits(const FrontParams &p, int dtype);   // FrontParams::logits pays if there is room for it
 int launch_front(const FrontParams &p, int dtype, hipStream_t st);
 int launch_remap(const RemapParams &p, hipStream_t st);
-bool remap_groups_ok(int T, int K, uint32_t flags);   // the batch is small enough for launch_remap_group (which reads w_in)
-int launch_remap_group(const RemapParams &p, const ScanParams &sp, const ScatterParams &cp, hipStream_t st);
+int launch_remap(const GivenRemapParams &p, hipStream_t st);
+bool remap_groups_ok(int T, int K, uint32_t flags);   // the batch is small enough for launch_remap_group
+int launch_remap_group(const GivenRemapParams &p, const ScanParams &sp, const ScatterParams &cp, hipStream_t st);
 int launch_count(const int32_t *ids, int T, int K, int E, int tile_tokens, int32_t *tile_counts, hipStream_t st);
 int launch_scan(const ScanParams &p, hipStream_t st);
 int launch_scatter(const ScatterParams &p, hipStream_t st);

@@ -137,10 +137,12 @@ def _ptr(t) -> Optional[int]:
     """Device (or host) address of a torch tensor / numpy array, None for None."""
     if t is None:
         return None
-    if hasattr(t, "data_ptr"):
-        assert t.is_contiguous(), "tensors must be contiguous"
-        return t.data_ptr()
-    return t.ctypes.data
+    try:
+        contiguous = t.is_contiguous()
+    except AttributeError:
+        return t.ctypes.data
+    assert contiguous, "tensors must be contiguous"
+    return t.data_ptr()
 
 
 _current_stream = None
@@ -369,8 +371,8 @@ def _rows_ptr(t, stride: int, width: int, rows: int) -> Optional[int]:
 
 def bm_add_adapters(desc: AdapterDesc, x, adapter, a, b, ranks, scale, base, y, workspace, stream: Optional[int] = None):
     """y = base + scale[s] * b[s] (a[s] x) with s = adapter[row]; x, base and y may be columns of wider matrices (desc's strides)."""
-    _check(load_library().bm_add_adapters(ctypes.byref(desc), _rows_ptr(x, desc.x_stride, desc.Kd, desc.rows), _ptr(adapter), _ptr(a), _ptr(b),
-                                          _ptr(ranks), _ptr(scale), _rows_ptr(base, desc.base_stride, desc.N, desc.rows),
-                                          _rows_ptr(y, desc.y_stride, desc.N, desc.rows), _ptr(workspace),
-                                          workspace.numel() * workspace.element_size(),
+    rows, width = desc.rows, desc.N                     # (a descriptor's field costs as much as a check)
+    _check(load_library().bm_add_adapters(ctypes.byref(desc), _rows_ptr(x, desc.x_stride, desc.Kd, rows), _ptr(adapter), _ptr(a), _ptr(b),
+                                          _ptr(ranks), _ptr(scale), _rows_ptr(base, desc.base_stride, width, rows),
+                                          _rows_ptr(y, desc.y_stride, width, rows), _ptr(workspace), workspace.nbytes,
                                           _stream() if stream is None else stream), "bm_add_adapters")

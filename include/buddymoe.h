@@ -502,7 +502,9 @@ typedef struct {
  * written; otherwise y must not overlap base or x (y == x is refused, BM_ERR_SHAPE).  Rows
  * of a strided array keep what lies between them.
  * Any sizes, strides and addresses are taken (4-byte addresses in fp32, 2-byte ones in
- * bf16); 16 bytes at a time where rows and addresses are multiples of that.
+ * bf16); 16 bytes at a time where rows and addresses are multiples of that.  Beyond 64
+ * rows the launches are sized for n, so arrays of hundreds of adapters cost time even
+ * where few are used.
  * Sums are fp32, a x is held in fp32 (bf16: where b multiplies it, as the sum of three bf16
  * values, its 24 bits, or for a bf16 y of two; an infinity in b then gives infinities or
  * NaN); y is rounded once.  Equal calls give equal bits; a row's y can differ in its last

@@ -4,8 +4,8 @@
 // Three launches: rows are grouped by adapter (chunks of 1024 rows, each on its own), u = A x of a tile of up to 64 rows of one
 // adapter (the reduction cut into parts over the chip), then B u is added to base on the way to y.  Up to 64 rows group themselves in
 // the other two, and a few rows of a small rank take one launch.  A and B are read once for each tile, x once, base and y once: many
-// rows are bound by base and y (8192 rows of 2048 -> 4096, rank 16: 134 MB in 28 us, a copy's rate, 46 us in all), few by launches
-// and trips to memory.  u is held in fp32.
+// rows are bound by base and y (8192 rows of 2048 -> 4096, rank 16: 134 MB in 29 us, a copy's rate; 46 us in all where the inputs lie in
+// the memory-side cache, 57 where they do not), few by launches and trips to memory.  u is held in fp32.
 #include "bm_adapters.h"
 
 namespace bm {
@@ -751,6 +751,9 @@ bool one_launch(const AdapterParams &p, bool f32, bool y_f32) {
 
 }  // namespace
 
+// The launches are sized for the adapters in the arrays, not for those that the rows turn out to use: what is not used is workgroups that
+// find no tile, and from about 256 adapters on fewer parts of the reduction.  2048 -> 4096, rank 16, in arrays of 6 / 64 / 512 / 1024 adapters, us: 8192
+// rows of 6 adapters 46 45 57 70, 1024 rows of one 19 20 32 29, 128 rows of 6 13 13 18 22; up to 64 rows the arrays do not matter (9).
 void plan_adapters(AdapterParams &p, bool f32) {
     p.chunks = (p.rows + ADAPTER_CHUNK - 1) / ADAPTER_CHUNK;
     const int rows = p.rows < ADAPTER_CHUNK ? p.rows : ADAPTER_CHUNK, keys = p.n + 1;

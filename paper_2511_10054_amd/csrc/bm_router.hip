@@ -476,7 +476,9 @@ constexpr int CHUNK = 16384;             // tokens whose logits lie in the scrat
 // From how many logits on the product is tiled: small | tiled product, us of the whole call.  bf16: 4096 -> 256 experts at 32 / 64 / 128 / 256
 // tokens 7.3 8.2 10.2 14.2 | 8.7 8.8 9.0 9.7, 2048 -> 128 at 64 / 128 / 256 6.6 7.7 9.9 | 7.1 7.5 8.0, 2048 -> 64 at 128 / 256 / 512
 // 6.1 7.1 9.1 | 6.7 7.0 7.4, 4096 -> 8 at 1024 / 2048 6.8 8.8 | 7.6 7.8.  fp32: 2048 -> 256 at 128 / 256 10.7 14.8 | 12.1 12.8,
-// 2048 -> 128 at 256 / 512 10.5 14.6 | 11.9 12.8, 1440 -> 60 at 512 / 1024 9.3 13.7 | 9.7 10.3.
+// 2048 -> 128 at 256 / 512 10.5 14.6 | 11.9 12.8, 1440 -> 60 at 512 / 1024 9.3 13.7 | 9.7 10.3.  The lines by logits alone: at the bf16 one
+// 4096 -> 256 (64 tokens) loses 0.6 us, 2048 -> 128, 2048 -> 64 and 4096 -> 8 win 0.2 to 1.0.  Rows or arrays off 16-byte addresses have no
+// tiled product: fp32, 1000 / 2048 tokens, 2047 -> 256 40 71 (2048 -> 256: 21 34), 1443 -> 60 12.3 19.1 (1440 -> 60: 10.1 11.5).
 bool wants_tiles(int T, int E, bool f32) { return (long long)T * E >= (f32 ? 40960 : 16384); }
 
 // A tiled product's workgroup takes one of the eight parts of the reduction, or of large batches two: half of the parts to write and to
